@@ -432,6 +432,152 @@ int loza_ssa_live_ranges_blocks(int64_t i, int64_t sink_blocks, int64_t local_bl
                                 int64_t *sink_end, int64_t *win_begin, int64_t *win_end);
 int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local_blocks, int64_t block);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * The step around the attention: what an engine that drafts tokens calls between one decode step and the next, all of
+ * it on the GPU (no lengths on the host), so that a step can be captured. The paper stretches its contexts with YaRN and
+ * measures its kernels inside such an engine (Training and Efficiency sections); it describes none of this, the definitions
+ * are the usual ones. A step: loza_ssa_step_tables, then in every layer loza_ssa_rope_append and loza_ssa_extend_tree
+ * (or loza_ssa_decode_paged, loza_ssa_extend_paged), then loza_ssa_verify_tree, and loza_ssa_keep_accepted for all layers.
+ *
+ * Trees. The tokens of a step are the nodes of a tree per sequence, at most LOZA_TREE_MAX_NODES of them, parents before their
+ * children. parents[b, r] is the parent of node r, an index below r; anything else: a node without a parent. Node 0 is the
+ * token that the last step ended with (its row is not in the cache yet), the others are drafts. A chain of drafts is
+ * the tree parents[r] = r - 1.
+ */
+#define LOZA_TREE_MAX_NODES 64
+#define LOZA_ROPE_MAX_DIM 1024
+
+/*
+ * Block tables, slots, positions and ancestor masks of a step, from the lengths of the requests.
+ *   cache_lens [B] int32: rows each request has in its cache     new_lens [B] int32: rows it is about to add, 0 .. n
+ *   parents [B, n] int32 or NULL: the step's tokens are trees (n <= LOZA_TREE_MAX_NODES) or the next tokens in a row
+ *   free_pages [num_free] int32, free_count [1] int32: pages nobody holds; the first free_count entries (at most num_free) are valid
+ *   block_table [B, max_pages_per_seq] int32: the pages that a request holds already (the first ceil(cache_len / page_size) entries of
+ *           its row) are read; the entries of the pages it needs beyond those are written, no others
+ *   granted [B] int32: new_lens, or 0 where the request cannot be served: pages are dealt out in the order of the requests,
+ *           from the end of the free list; one whose need, with those of all requests before it (served or not), exceeds free_count gets none (one that needs
+ *           no new page is always served), nor does one with lengths that are negative, beyond n, or beyond max_pages_per_seq
+ *           pages (these take nothing from the others)
+ *   seqlens [B] int32: cache_lens + granted, as the decode and extend calls take it
+ *   positions, slots [B, n] int32: the position of each token and the cache row (page * page_size + row in the page) it goes to;
+ *           -1 for rows without a token (of requests that were not served, too), slots also where the table holds a page outside [0, num_pages).
+ *           Trees: row r is node r (r < granted), at row cache_len + r and position cache_len + the number of its
+ *           ancestors. No trees: the last `granted` of the n rows, as loza_ssa_extend_paged counts them (row r at
+ *           position seqlens - n + r).
+ *   masks [B, n] int64 (NULL without parents): bit a of masks[b, r] says that node r sees node a: its ancestors and itself; 0
+ *           for rows without a token
+ *   free_left [1] int32: valid entries of free_pages that are left
+ * page_size: a power of two >= 32; num_pages * page_size < 2^31. granted, seqlens and free_left must not be the arrays they
+ * are made from (LOZA_ERR_SHAPE). The call is repeatable: it changes none of its inputs but those entries of block_table.
+ */
+int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                         const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                         int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                         int32_t *slots, int64_t *masks, int32_t *free_left, void *stream);
+
+/*
+ * Rotary positions, and their gradient. Pair k of the columns [rot_begin, rot_begin + rot_dim) of a head at position i,
+ * (a, b) -> mscale (a cos t - b sin t, a sin t + b cos t), t = i * freq[k]; inverse != 0: by -t, which is the gradient of
+ * the rotation (of x from that of out), and undoes it where mscale is 1.
+ *   x, out [T, H, d]: element (t, h, c) at t * token stride + h * head stride + c (strides in elements, >= 0; the places of out must
+ *           not overlap). out == x with the same strides: in place; other overlaps are not allowed. Columns outside the rotary ones are
+ *           copied.
+ *   positions [T] int32: >= 0; a token with a negative one is padding, its row of out is left as it is
+ *   freq [rot_dim / 2] float64, radians per position (loza_ssa_rope_frequencies); rot_dim even, 2 .. LOZA_ROPE_MAX_DIM
+ *   interleaved != 0: pair k is columns 2 k and 2 k + 1, else k and k + rot_dim / 2 (from rot_begin)
+ * bf16 (loza_ssa_rope) or fp32. Base pointers need only be aligned to their elements; 16 bytes for them, the strides, d, rot_begin and (half of, where
+ * pairs are not interleaved) rot_dim is several times faster. Angles in 64 bits and more (exact to 2^-24 of a turn at any
+ * position), sine and cosine in fp32, one rounding of each result.
+ */
+int loza_ssa_rope(const void *x, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                  int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int rot_begin, int rot_dim,
+                  int interleaved, int inverse, float mscale, void *stream);
+int loza_ssa_rope_f32(const float *x, const int32_t *positions, const double *freq, float *out, int64_t T, int H, int d,
+                      int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int rot_begin, int rot_dim,
+                      int interleaved, int inverse, float mscale, void *stream);
+
+/*
+ * The same for the queries and keys of a step, whose keys (rotated) and values (as they are) go to the cache in the same launch.
+ *   q [T, Hq, d_q] -> q_out (strided as above, q_rot_begin; both NULL: keys and values only)
+ *   k [T, Hkv, d_k] (strided, k_rot_begin) -> row slots[t] of k_rows [cache_rows, Hkv, d_k] (a paged or contiguous cache, whole rows dense)
+ *   v [T, Hkv, d_v] (strided) -> row slots[t] of v_rows [cache_rows, Hkv, d_v]; both NULL where the values are part of the keys
+ *   slots [T] int32: a token whose slot is outside [0, cache_rows), or whose position is negative, is not written to the cache
+ *           (a rotated query needs the position only). No two tokens may have the same slot.
+ */
+int loza_ssa_rope_append(const void *q, const void *k, const void *v, const int32_t *positions, const int32_t *slots, const double *freq,
+                         void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q, int d_k, int d_v,
+                         int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                         int64_t v_token, int64_t v_head, int64_t cache_rows, int q_rot_begin, int k_rot_begin, int rot_dim,
+                         int interleaved, float mscale, void *stream);
+int loza_ssa_rope_append_f32(const float *q, const float *k, const float *v, const int32_t *positions, const int32_t *slots, const double *freq,
+                             float *q_out, float *k_rows, float *v_rows, int64_t T, int Hq, int Hkv, int d_q, int d_k, int d_v,
+                             int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                             int64_t v_token, int64_t v_head, int64_t cache_rows, int q_rot_begin, int k_rot_begin, int rot_dim,
+                             int interleaved, float mscale, void *stream);
+
+/*
+ * Host-only (ours). Frequencies for contexts stretched by `factor` (the paper's YaRN, Training section): f_k = base^(-2k / rot_dim)
+ * turns original_context * f_k / 2 pi times over the context that was trained; pairs of fewer than slow_turns (usually 1) are divided by the
+ * factor, pairs of more than fast_turns (usually 32) are kept, those between are mixed linearly in their turns.
+ * *mscale = 0.1 ln(factor) + 1, what queries and keys are scaled by (a model that has it in its softmax scale passes 1 instead).
+ * factor = 1: plain frequencies, *mscale = 1, the last four arguments before freq unused.
+ */
+int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t original_context, double slow_turns,
+                              double fast_turns, double *freq, float *mscale);
+
+/*
+ * Attention of a tree of drafted tokens over a cache that already holds their rows: loza_ssa_extend_with_workspace with the
+ * queries of a tree in the place of consecutive ones.
+ *   block_table == NULL: k, v [B, S_max, Hkv, d] (num_pages, page_size, max_pages_per_seq unused), else pages (S_max unused)
+ *   q [B, n, Hq, d_qk] bf16, out [B, n, Hq, d_v] bf16, lse [B, Hq, n] fp32; 1 <= n <= LOZA_TREE_MAX_NODES, n <= S_max
+ *   seqlens [B] int32: valid cache rows, the nodes' rows included, which are the last tree_lens[b] of them (a length beyond the cache is cut to it)
+ *   tree_lens [B] int32: nodes of each tree, cut to [0, n] and to seqlens. Rows r >= tree_lens[b]
+ *           give out = 0, lse = -inf. Cache rows at or beyond seqlens[b] are never read.
+ *   masks [B, n] int64: the nodes that node r sees (loza_ssa_step_tables makes them; its own bit has to be set if it is
+ *           to see itself; bits at or beyond tree_lens[b] are ignored). With P = seqlens[b] - tree_lens[b]: node r sits at position
+ *           i = P + popcount(mask) - 1 and sees cache row j < P if j is live for position i, and the node of
+ *           the k-th set bit (from 0) if position P + k is. A chain's masks (bits 0 .. r) give what loza_ssa_extend
+ *           gives. A mask of 0: the row sees nothing, out = 0, lse = -inf.
+ *   pattern, supported shapes, numerics: as loza_ssa_extend_blocks (block = 1: token-granular)
+ *   workspace: as loza_ssa_extend_with_workspace, loza_ssa_extend_tree_workspace_bytes of it; NULL: no workgroups share keys
+ */
+int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int32_t *block_table, const int32_t *seqlens,
+                         const int32_t *tree_lens, const int64_t *masks, void *out, float *lse, int B, int Hq, int Hkv,
+                         int64_t S_max, int64_t num_pages, int page_size, int max_pages_per_seq, int n, int d_qk, int d_v,
+                         int64_t sink_blocks, int64_t local_blocks, int64_t block, float scale, void *workspace,
+                         size_t workspace_bytes, void *stream);
+size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
+                                            int64_t sink_blocks, int64_t local_blocks, int64_t block);
+
+/*
+ * Which drafts hold, and the token after them, from given random numbers, such that tokens are distributed as the target's
+ * (recursive rejection sampling).
+ *   target [B, n, V] fp32: probabilities after node r     draft [B, n, V] fp32: those that the children of node r were drawn from,
+ *           independently; NULL: the drafts were not drawn at random
+ *   tokens, parents [B, n] int32 (a node with a token outside [0, V) is skipped; tokens[b, 0] is not read), tree_lens [B] int32 (cut to [0, n])
+ *   u_accept [B, n], u_next [B] fp32 in [0, 1)
+ * From node 0 on: w = target, s = 1; the children x of the node are tried in order. Taken if u_accept q(x) s < w(x): on from there.
+ * Else w = max(w - s q, 0), s = the sum of w. (Without draft q(x) = 1, w loses x, s the w(x).) Where no child is taken: the next token is
+ * the first x whose w(0) + .. + w(x) exceeds u_next times the sum of all (w = target again if nothing is left of w).
+ *   path [B, n] int32: nodes on the path, node 0 first, then -1     path_lens [B] int32: how many (0 for an empty tree)
+ *   next_token [B] int32: the token after the path; -1 for an empty tree or a target row without weight
+ *   workspace: loza_ssa_verify_tree_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
+ * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30. Sums and decisions in fp64, always in the same order.
+ */
+int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,
+                         const float *u_accept, const float *u_next, int32_t *path, int32_t *path_lens, int32_t *next_token,
+                         int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream);
+size_t loza_ssa_verify_tree_workspace_bytes(int B, int n, int V);
+
+/*
+ * The rows of the accepted path to where a next step expects them: row slots[b, path[b, i]] becomes row slots[b, i] for all i < path_lens[b]
+ * (the rows as they were before the call), in each of n_layers caches k_rows [n_layers, cache_rows, k_row_bytes], and v_rows likewise (NULL:
+ * none). The request then has path_lens[b] rows more in its cache. Entries of path and slots outside their ranges are skipped; slots that the call
+ * moves rows to or from must belong to one b. Row sizes: multiples of 16 bytes. B * n_layers <= 65535.
+ */
+int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, const int32_t *path, const int32_t *path_lens, int B, int n,
+                           int n_layers, int64_t cache_rows, int64_t k_row_bytes, int64_t v_row_bytes, void *stream);
+
 /* Host-only (ours). Static string naming a status code. */
 const char *loza_status_str(int status);
 

@@ -10,6 +10,7 @@
 #include "../../include/loza_ssa.h"
 #include "ssa_kernels.h"
 #include "ssa_schedule.h"
+#include "ssa_step.h"
 
 // Scratch memory of loza_ssa_decode_static: the split kernel's partial results, in the place of a
 // caller's workspace. One copy per GPU, at an address of its own on each; the name below is only a
@@ -336,7 +337,8 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
                         int64_t sink, int64_t local, int64_t block, bool blocks, float scale, void *stream,
                         float *out_f32 = nullptr, bool validate_only = false,
                         const int32_t *seqlens = nullptr, int64_t q_len = 0, const Paging *paging = nullptr,
-                        bool scratch = false, void *workspace = nullptr, size_t workspace_bytes = 0)
+                        bool scratch = false, void *workspace = nullptr, size_t workspace_bytes = 0,
+                        const int32_t *tree_lens = nullptr, const int64_t *tree_masks = nullptr)
 {
     // seqlens != nullptr: "extend" form, q_len queries per sequence against a cache of S rows
     // (with a paging description: of max_pages * page_size rows behind a block table); scratch: the caller offers
@@ -390,6 +392,10 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
         if (paging) {
             p.block_table = paging->block_table;
             p.page_shift = page_shift; p.max_pages = paging->max_pages; p.num_pages = (int)paging->num_pages;
+        }
+        if (tree_masks) {
+            p.tree_lens = tree_lens; p.tree_masks = tree_masks;
+            return loza::launch_tree_plain(p, d_qk, alias, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
         }
         if (few_rows) return loza::launch_rows_bf16(p, d_qk, d_v, alias, false, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
         return loza::launch_extend_bf16(p, d_qk, d_v, alias, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
@@ -1097,6 +1103,227 @@ int loza_ssa_decode_blocks(const void *q, const void *kcache, const void *vcache
 {
     return decode_bf16(q, kcache, vcache, seqlens, out, lse, B, Hq, Hkv, S_max, d_qk, d_v, sink_blocks, local_blocks,
                        block, true, scale, workspace, workspace_bytes, stream);
+}
+
+// ---- the step around the attention ----------------------------------------------------------------------
+
+int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int32_t *block_table, const int32_t *seqlens,
+                         const int32_t *tree_lens, const int64_t *masks, void *out, float *lse, int B, int Hq, int Hkv,
+                         int64_t S_max, int64_t num_pages, int page_size, int max_pages_per_seq, int n, int d_qk, int d_v,
+                         int64_t sink_blocks, int64_t local_blocks, int64_t block, float scale, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    if (!seqlens || !tree_lens || !masks) return LOZA_ERR_NULL;
+    if (n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(tree_lens) & 3u) || (reinterpret_cast<uintptr_t>(masks) & 7u)) return LOZA_ERR_ALIGN;
+    const Paging pg{block_table, num_pages, page_size, max_pages_per_seq};
+    return prefill_bf16(q, k, v, out, lse, B, Hq, Hkv, block_table ? 1 : S_max, d_qk, d_v, sink_blocks, local_blocks, block, true,
+                        scale, stream, nullptr, false, seqlens, n, block_table ? &pg : nullptr, workspace != nullptr, workspace, workspace_bytes,
+                        tree_lens, masks);
+}
+
+size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
+                                            int64_t sink_blocks, int64_t local_blocks, int64_t block)
+{
+    if (n > LOZA_TREE_MAX_NODES) return 0;
+    return loza_ssa_extend_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, sink_blocks, local_blocks, block);
+}
+
+int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                         const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                         int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                         int32_t *slots, int64_t *masks, int32_t *free_left, void *stream)
+{
+    if (!cache_lens || !new_lens || !free_count || !granted || !seqlens || !positions || !slots || !free_left) return LOZA_ERR_NULL;
+    if (!free_pages && num_free > 0) return LOZA_ERR_NULL;
+    if ((parents == nullptr) != (masks == nullptr)) return LOZA_ERR_NULL;
+    if (B < 1 || n < 1 || num_free < 0 || num_free > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (parents && n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    int shift = 0;
+    int64_t capacity = 0;
+    if (int rc = check_paging(Paging{block_table, num_pages, page_size, max_pages_per_seq}, &shift, &capacity)) return rc;
+    if (num_pages * page_size > 2147483647LL) return LOZA_ERR_SHAPE;   // slots are 32-bit row numbers
+    if ((int64_t)n > 65535LL * 1024) return LOZA_ERR_SHAPE;
+    // a workgroup reads what another's results would be written over
+    if (granted == new_lens || seqlens == cache_lens || free_left == free_count) return LOZA_ERR_SHAPE;
+    for (const void *ptr : {(const void *)cache_lens, (const void *)new_lens, (const void *)parents, (const void *)free_pages, (const void *)free_count,
+                            (const void *)granted, (const void *)seqlens, (const void *)positions, (const void *)slots, (const void *)free_left})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(masks) & 7u) return LOZA_ERR_ALIGN;
+    loza::TablesParams p{};
+    p.cache_lens = cache_lens; p.new_lens = new_lens; p.parents = parents; p.free_pages = free_pages; p.free_count = free_count;
+    p.block_table = block_table; p.granted = granted; p.seqlens = seqlens; p.positions = positions; p.slots = slots;
+    p.masks = masks; p.free_left = free_left;
+    p.B = B; p.n = n; p.page_shift = shift; p.max_pages = max_pages_per_seq; p.num_free = num_free; p.num_pages = num_pages;
+    return loza::launch_step_tables(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t original_context, double slow_turns,
+                              double fast_turns, double *freq, float *mscale)
+{
+    if (!freq || !mscale) return LOZA_ERR_NULL;
+    if (rot_dim < 2 || rot_dim > LOZA_ROPE_MAX_DIM || (rot_dim & 1)) return LOZA_ERR_SHAPE;
+    if (!(base > 1.0) || isinf(base) || !(factor >= 1.0) || isinf(factor)) return LOZA_ERR_SHAPE;
+    if (factor > 1.0 && (original_context < 1 || !(slow_turns >= 0.0) || !(fast_turns > slow_turns) || isinf(fast_turns))) return LOZA_ERR_SHAPE;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = pow(base, -2.0 * i / rot_dim);
+        double keep = 1.0;                                 // share of the frequency that is not stretched
+        if (factor > 1.0) {
+            const double turns = (double)original_context * f / 6.28318530717958647693;
+            keep = (turns - slow_turns) / (fast_turns - slow_turns);
+            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        }
+        freq[i] = f / factor * (1.0 - keep) + f * keep;
+    }
+    *mscale = factor > 1.0 ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return LOZA_OK;
+}
+
+// Checks one tensor of heads: pointers to whole elements, and (out) places that do not overlap.
+static int check_heads(const loza::RopeHeads &r, int64_t T, int rot, int es, bool out_strided)
+{
+    if (!r.x || !r.out) return LOZA_ERR_NULL;
+    if (r.H < 1 || r.d < 1 || r.rot_begin < 0 || (int64_t)r.rot_begin + rot > r.d) return LOZA_ERR_SHAPE;
+    if (r.x_token < 0 || r.x_head < 0) return LOZA_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(r.x) | reinterpret_cast<uintptr_t>(r.out)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
+    if (!out_strided) return LOZA_OK;
+    const int64_t t = r.out_token, h = r.out_head, big = INT64_MAX / 4;
+    if (t < 0 || h < 0 || t > big / T || h > big / r.H || r.x_token > big / T || r.x_head > big / r.H) return LOZA_ERR_SHAPE;
+    const bool heads_inside = (r.H == 1 || h >= r.d) && (T == 1 || t >= (r.H - 1) * h + r.d);
+    const bool tokens_inside = (T == 1 || t >= r.d) && (r.H == 1 || h >= (T - 1) * t + r.d);
+    if (!heads_inside && !tokens_inside) return LOZA_ERR_SHAPE;
+    if (r.x == r.out && ((T > 1 && r.x_token != t) || (r.H > 1 && r.x_head != h))) return LOZA_ERR_SHAPE;
+    return LOZA_OK;
+}
+
+static int check_rope(const loza::RopeParams &p)
+{
+    if (!p.positions || !p.freq) return LOZA_ERR_NULL;
+    if (p.T < 1 || p.T > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (p.rot < 2 || p.rot > LOZA_ROPE_MAX_DIM || (p.rot & 1)) return LOZA_ERR_SHAPE;
+    if (!(p.mscale == p.mscale) || isinf(p.mscale)) return LOZA_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(p.positions) & 3u) || (reinterpret_cast<uintptr_t>(p.freq) & 7u)) return LOZA_ERR_ALIGN;
+    return LOZA_OK;
+}
+
+static int rope(const void *x, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int rot_begin, int rot_dim,
+                int interleaved, int inverse, float mscale, int es, void *stream)
+{
+    loza::RopeParams p{};
+    p.q = {x, out, x_token, x_head, out_token, out_head, H, d, rot_begin};
+    p.positions = positions; p.freq = freq; p.T = T; p.rot = rot_dim;
+    p.interleaved = interleaved != 0; p.inverse = inverse != 0; p.mscale = mscale;
+    if (int rc = check_rope(p)) return rc;
+    if (int rc = check_heads(p.q, T, rot_dim, es, true)) return rc;
+    return loza::launch_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_rope(const void *x, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                  int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int rot_begin, int rot_dim,
+                  int interleaved, int inverse, float mscale, void *stream)
+{
+    return rope(x, positions, freq, out, T, H, d, x_token, x_head, out_token, out_head, rot_begin, rot_dim, interleaved, inverse, mscale, 2, stream);
+}
+
+int loza_ssa_rope_f32(const float *x, const int32_t *positions, const double *freq, float *out, int64_t T, int H, int d,
+                      int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int rot_begin, int rot_dim,
+                      int interleaved, int inverse, float mscale, void *stream)
+{
+    return rope(x, positions, freq, out, T, H, d, x_token, x_head, out_token, out_head, rot_begin, rot_dim, interleaved, inverse, mscale, 4, stream);
+}
+
+static int rope_append(const void *q, const void *k, const void *v, const int32_t *positions, const int32_t *slots, const double *freq,
+                       void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q, int d_k, int d_v,
+                       int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                       int64_t v_token, int64_t v_head, int64_t cache_rows, int q_rot_begin, int k_rot_begin, int rot_dim,
+                       int interleaved, float mscale, int es, void *stream)
+{
+    loza::RopeParams p{};
+    if (q) p.q = {q, q_out, q_token, q_head, q_out_token, q_out_head, Hq, d_q, q_rot_begin};
+    p.k = {k, k_rows, k_token, k_head, (int64_t)Hkv * d_k, d_k, Hkv, d_k, k_rot_begin};
+    p.v = v; p.v_rows = v_rows; p.v_token = v_token; p.v_head = v_head; p.d_v = d_v;
+    p.positions = positions; p.slots = slots; p.freq = freq; p.T = T; p.cache_rows = cache_rows; p.rot = rot_dim;
+    p.interleaved = interleaved != 0; p.mscale = mscale;
+    if (!slots || (q == nullptr) != (q_out == nullptr) || (v == nullptr) != (v_rows == nullptr)) return LOZA_ERR_NULL;
+    if (int rc = check_rope(p)) return rc;
+    if (q) { if (int rc = check_heads(p.q, T, rot_dim, es, true)) return rc; }
+    if (int rc = check_heads(p.k, T, rot_dim, es, false)) return rc;
+    if (k == k_rows || cache_rows < 1 || cache_rows > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(slots) & 3u) return LOZA_ERR_ALIGN;
+    if (v) {
+        if (d_v < 1 || v_token < 0 || v_head < 0 || v == v_rows) return LOZA_ERR_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(v_rows)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
+    }
+    return loza::launch_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_rope_append(const void *q, const void *k, const void *v, const int32_t *positions, const int32_t *slots, const double *freq,
+                         void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q, int d_k, int d_v,
+                         int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                         int64_t v_token, int64_t v_head, int64_t cache_rows, int q_rot_begin, int k_rot_begin, int rot_dim,
+                         int interleaved, float mscale, void *stream)
+{
+    return rope_append(q, k, v, positions, slots, freq, q_out, k_rows, v_rows, T, Hq, Hkv, d_q, d_k, d_v, q_token, q_head, q_out_token, q_out_head,
+                       k_token, k_head, v_token, v_head, cache_rows, q_rot_begin, k_rot_begin, rot_dim, interleaved, mscale, 2, stream);
+}
+
+int loza_ssa_rope_append_f32(const float *q, const float *k, const float *v, const int32_t *positions, const int32_t *slots, const double *freq,
+                             float *q_out, float *k_rows, float *v_rows, int64_t T, int Hq, int Hkv, int d_q, int d_k, int d_v,
+                             int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                             int64_t v_token, int64_t v_head, int64_t cache_rows, int q_rot_begin, int k_rot_begin, int rot_dim,
+                             int interleaved, float mscale, void *stream)
+{
+    return rope_append(q, k, v, positions, slots, freq, q_out, k_rows, v_rows, T, Hq, Hkv, d_q, d_k, d_v, q_token, q_head, q_out_token, q_out_head,
+                       k_token, k_head, v_token, v_head, cache_rows, q_rot_begin, k_rot_begin, rot_dim, interleaved, mscale, 4, stream);
+}
+
+// Sizes of a verification that a call accepts; fills in the plan.
+static int check_verify(loza::VerifyParams &p, int B, int n, int V, bool draft)
+{
+    if (B < 1 || B > 65535 || n < 1 || n > LOZA_TREE_MAX_NODES || V < 1 || V > 1 << 30) return LOZA_ERR_SHAPE;
+    p.B = B; p.n = n; p.V = V;
+    loza::verify_plan(p, draft);
+    return LOZA_OK;
+}
+
+size_t loza_ssa_verify_tree_workspace_bytes(int B, int n, int V)
+{
+    loza::VerifyParams p{};
+    if (check_verify(p, B, n, V, true) != LOZA_OK) return 0;
+    return (size_t)B * p.rounds * p.slices * sizeof(double);
+}
+
+int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,
+                         const float *u_accept, const float *u_next, int32_t *path, int32_t *path_lens, int32_t *next_token,
+                         int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!target || !tokens || !parents || !tree_lens || !u_accept || !u_next || !path || !path_lens || !next_token) return LOZA_ERR_NULL;
+    loza::VerifyParams p{};
+    if (int rc = check_verify(p, B, n, V, draft != nullptr)) return rc;
+    if (!workspace || workspace_bytes < loza_ssa_verify_tree_workspace_bytes(B, n, V)) return LOZA_ERR_WORKSPACE;
+    for (const void *ptr : {(const void *)target, (const void *)draft, (const void *)tokens, (const void *)parents, (const void *)tree_lens,
+                            (const void *)u_accept, (const void *)u_next, (const void *)path, (const void *)path_lens, (const void *)next_token})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
+    p.target = target; p.draft = draft; p.tokens = tokens; p.parents = parents; p.tree_lens = tree_lens; p.u_accept = u_accept; p.u_next = u_next;
+    p.path = path; p.path_lens = path_lens; p.next_token = next_token; p.partial = (double *)workspace;
+    return loza::launch_verify_tree(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, const int32_t *path, const int32_t *path_lens, int B, int n,
+                           int n_layers, int64_t cache_rows, int64_t k_row_bytes, int64_t v_row_bytes, void *stream)
+{
+    if (!k_rows || !slots || !path || !path_lens) return LOZA_ERR_NULL;
+    if (B < 1 || n < 1 || n > LOZA_TREE_MAX_NODES || n_layers < 1 || (int64_t)B * n_layers > 65535) return LOZA_ERR_SHAPE;
+    const int64_t most = (int64_t)1 << 24;     // bytes of a row
+    if (cache_rows < 1 || cache_rows > 2147483647LL || k_row_bytes < 16 || k_row_bytes > most || (k_row_bytes & 15)) return LOZA_ERR_SHAPE;
+    if (v_rows && (v_row_bytes < 16 || v_row_bytes > most || (v_row_bytes & 15) || v_rows == k_rows)) return LOZA_ERR_SHAPE;
+    if (!aligned16(k_rows) || !aligned16(v_rows)) return LOZA_ERR_ALIGN;
+    for (const void *ptr : {(const void *)slots, (const void *)path, (const void *)path_lens})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    loza::KeepParams p{(char *)k_rows, (char *)v_rows, slots, path, path_lens, B, n, n_layers, cache_rows, k_row_bytes, v_rows ? v_row_bytes : 0};
+    return loza::launch_keep_accepted(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }
 
 }  // extern "C"

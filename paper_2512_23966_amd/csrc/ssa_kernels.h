@@ -36,6 +36,9 @@ struct FwdParams {
     int rt_begin;      // first of them
     int n_splits;      // decode and extend: workgroups that share the keys of a row (1: no partial results)
     int q_len;         // extend prefill: queries per sequence (0: plain prefill); keys valid up to seqlens[b]
+    // a tree of drafted tokens (extend, else nullptr): the nodes of each sequence, q_len at most, and what each sees (ssa_tree.h)
+    const int32_t *tree_lens;
+    const int64_t *tree_masks;
     int all_precise;   // tile kernel, prefill / extend: every tile takes the two-term pass (set by the launcher from the pattern)
     int exact_tiles;   // tile kernel: tiles over which the reference maximum is the exact running maximum
     float lazy_log2;   // afterwards it moves only when exceeded by this much (log2 units)
@@ -68,6 +71,7 @@ bool d128_tiles_pay(int B, int Hkv, int G, int64_t queries, int64_t S, int n_sin
 // Few query rows (ssa_rows.hip): prefill (seqlens null), extend or decode (q_len = 1; n_splits key splits
 // and a merge; weights that are not rounded at all).
 hipError_t launch_rows_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, bool decode, hipStream_t stream);
+hipError_t launch_tree_plain(const FwdParams &p, int d_qk, bool alias, hipStream_t stream);
 // A prefill or extend of `rows` query rows per (batch, key head) is few rows when its groups of 16 rows make
 // at most two rounds of the 256 compute units. A round of the row kernel and one of the tile kernel (128 rows
 // a workgroup) cost, at window 8192 of the wide shape, 165 and 405 us (d = 128, window 4096: 51 and 152):

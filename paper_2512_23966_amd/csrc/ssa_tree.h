@@ -1,0 +1,59 @@
+// A tree of drafted tokens as the queries of an extend: which keys a node sees.
+//
+// The nodes of sequence b are the last tree_lens[b] of its seqlens[b] cache rows, P rows come before them. Node r carries a mask: bit
+// a says that it sees node a. Its position is P plus the nodes it sees, itself not counted; of the P rows it sees what the
+// pattern gives that position, and of the nodes of its mask, the k-th of which sits at position P + k, those that are in the
+// sink or in the window.
+#ifndef LOZA_SSA_TREE_H
+#define LOZA_SSA_TREE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ssa_device.h"
+#include "ssa_kernels.h"
+
+namespace loza {
+
+struct TreeSpan {
+    int64_t L, P;        // valid cache rows, and those before the tree
+    int nodes;
+};
+__device__ __forceinline__ TreeSpan tree_span(const FwdParams &p, int b)
+{
+    TreeSpan s;
+    s.L = (int64_t)p.seqlens[b] < p.S ? (int64_t)p.seqlens[b] : p.S;
+    if (s.L < 0) s.L = 0;
+    int n = p.tree_lens[b];
+    n = n < 0 ? 0 : n < p.q_len ? n : p.q_len;
+    s.nodes = n < s.L ? n : (int)s.L;
+    s.P = s.L - s.nodes;
+    return s;
+}
+
+struct TreeRow {
+    uint64_t mask;       // nodes that the row sees
+    int w_lo;            // first key of its window
+    bool seen;           // false: padding, or a node without a mask: it sees nothing
+};
+__device__ __forceinline__ TreeRow tree_row(const FwdParams &p, const TreeSpan &s, int b, int r)
+{
+    TreeRow t;
+    const uint64_t there = s.nodes < 64 ? ((uint64_t)1 << s.nodes) - 1 : ~(uint64_t)0;
+    t.mask = r < s.nodes ? (uint64_t)p.tree_masks[(int64_t)b * p.q_len + r] & there : 0;
+    t.seen = t.mask != 0;
+    const int i = (int)s.P + __popcll(t.mask) - 1;
+    t.w_lo = window_begin_of(i < 0 ? 0 : i, p.window, p.block);
+    // nodes of the path whose positions are behind the window (few windows are shorter than a path) and not in the sink
+    const int cut = t.w_lo - (int)s.P, sink = p.n_sink - (int)s.P;
+    if (cut > 0) {
+        uint64_t keep = 0, left = t.mask;
+        for (int k = 0; left != 0; ++k, left &= left - 1)
+            if (k >= cut || k < sink) keep |= left & -left;
+        t.mask = keep;
+    }
+    return t;
+}
+
+}  // namespace loza
+#endif
