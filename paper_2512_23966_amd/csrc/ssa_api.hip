@@ -393,10 +393,7 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
             p.block_table = paging->block_table;
             p.page_shift = page_shift; p.max_pages = paging->max_pages; p.num_pages = (int)paging->num_pages;
         }
-        if (tree_masks) {
-            p.tree_lens = tree_lens; p.tree_masks = tree_masks;
-            return loza::launch_tree_plain(p, d_qk, alias, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
-        }
+        p.tree_lens = tree_lens; p.tree_masks = tree_masks;
         if (few_rows) return loza::launch_rows_bf16(p, d_qk, d_v, alias, false, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
         return loza::launch_extend_bf16(p, d_qk, d_v, alias, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
     }

@@ -43,6 +43,7 @@
 #include "ssa_direct.h"
 #include "ssa_kernels.h"
 #include "ssa_schedule.h"
+#include "ssa_tree.h"
 
 namespace loza {
 
@@ -120,8 +121,9 @@ struct TileCfg {
 // One pass over one workgroup tile. PRECISE: P goes to the value phase as two bf16 terms. Returns
 // true (the same in every wave) when the tile has been left unwritten for a PRECISE pass. SPLIT (extend): the
 // workgroup takes every n_splits-th live key tile and leaves fp32 partial results, as a decode's does; which rows have
-// a large result is not known before these have been added up, so all of them are PRECISE.
-template <int DQK, int DV, int RB, bool ALIAS, bool DECODE, bool PRECISE, bool OUTF32, bool EXT, bool SPLIT = false>
+// a large result is not known before these have been added up, so all of them are PRECISE. TREE (extend): the queries are the
+// nodes of a tree of drafted tokens (ssa_tree.h): keys before the tree are masked by position, those of the tree by 64 bits a row.
+template <int DQK, int DV, int RB, bool ALIAS, bool DECODE, bool PRECISE, bool OUTF32, bool EXT, bool SPLIT = false, bool TREE = false>
 static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *smem)
 {
     using C = TileCfg<DQK, DV, RB, ALIAS, DECODE>;
@@ -185,19 +187,29 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
     const int64_t my_row = r0 + wr * 32 + ln;
     const int64_t my_row_c = my_row < R ? my_row : R - 1;
     const int r_row = DECODE ? 0 : (int)row_position(my_row_c, G);           // index of the query among the Sq
-    const int i_row = DECODE ? (int)(L - 1) : (int)(pos0 + r_row);
-    const int i_min = DECODE ? (int)(L - 1) : (int)(pos0 + row_position(r0, G));
-    const int i_max = DECODE ? (int)(L - 1) : (int)(pos0 + row_position((r0 + M - 1 < R) ? r0 + M - 1 : R - 1, G));
+    TreeSpan span{};
+    TreeRow node{};
+    if constexpr (TREE) {
+        span = tree_span(p, b);
+        node = tree_row(p, span, b, r_row);
+    }
+    const bool padding = TREE && row_position(r0, G) >= span.nodes;    // (no node among these rows)
+    // (a tree: i_row and i_min are the last key before it, the first window is that of position P, the last that of a chain's end)
+    const int i_row = DECODE ? (int)(L - 1) : TREE ? (node.seen ? (int)span.P - 1 : kNothing) : (int)(pos0 + r_row);
+    const int i_min = DECODE ? (int)(L - 1) : TREE ? (int)span.P - 1 : (int)(pos0 + row_position(r0, G));
+    const int i_max = DECODE ? (int)(L - 1) : TREE ? (padding ? -1 : (int)span.L - 1)
+                                                   : (int)(pos0 + row_position((r0 + M - 1 < R) ? r0 + M - 1 : R - 1, G));
+    const int i_low = TREE ? (int)span.P : i_min;
     // Tiles among the first positions, and every tile of a pattern that leaves all rows few live keys,
     // take the two-term pass right away.
-    if (!DECODE && !PRECISE && (p.all_precise || i_min < kPrecisePositions)) return true;
+    if (!DECODE && !PRECISE && (p.all_precise || i_low < kPrecisePositions)) return true;
 
     bf16x8 qf[DQK / 16];
 
     // ---- live key tiles: sink tiles [0, nA), then window tiles [wt0, wt0 + nB) -------------------
     const int sink_end = i_max < 0 ? 0 : (n_sink < i_max + 1 ? n_sink : i_max + 1);
-    const int win_begin = window_begin(i_min < 0 ? 0 : i_min);
-    const int w_lo_row = window_begin(i_row), w_lo_max = window_begin(i_max);
+    const int win_begin = window_begin(i_low < 0 ? 0 : i_low);
+    const int w_lo_row = TREE ? node.w_lo : window_begin(i_row), w_lo_max = window_begin(i_max);
     int nA = (sink_end + N - 1) / N;
     const int wt0 = win_begin / N, wt1 = i_max / N;
     int nB;
@@ -419,10 +431,12 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
         const bool interior = (j0 + N - 1 <= i_min) && ((j0 + N - 1 < n_sink) || (j0 >= w_lo_max));
         if (!interior) {
             const int jb = j0 + 4 * lh;
+            const uint32_t nodes = TREE ? tree_bits(node.mask, jb - (int)span.P) : 0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int j = jb + 8 * (e >> 2) + (e & 3);
-                const bool ok = (j <= i_row) & ((j < n_sink) | (j >= w_lo_row));
+                bool ok = (j <= i_row) & ((j < n_sink) | (j >= w_lo_row));
+                if constexpr (TREE) ok |= (nodes >> (8 * (e >> 2) + (e & 3))) & 1;
                 s[e] = ok ? s[e] : LOZA_NEG_INF;
             }
         }
@@ -844,6 +858,10 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
     }
 
     // ---- epilogue ----------------------------------------------------------------------------------
+    if (TREE && i_row == kNothing) {               // (tiles that take no mask have been added to its sums)
+        m_ref = LOZA_NEG_INF;
+        l_run = lr_run = 0.f;
+    }
     if (scorer) {
         const float l_lane = l_run + xor32(l_run);
         const float lr_lane = lr_run + xor32(lr_run);
@@ -998,17 +1016,17 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
 // Prefill / extend: every tile is computed with P rounded to bf16 once; a tile that cannot afford
 // that (few live keys per row, or a result large enough that its own rounding fills the error
 // budget) is computed with two-term P instead. Decode, and an extend whose keys are split: one pass.
-template <int DQK, int DV, int RB, bool ALIAS, bool DECODE, bool OUTF32 = false, bool EXT = false, bool SPLIT = false>
+template <int DQK, int DV, int RB, bool ALIAS, bool DECODE, bool OUTF32 = false, bool EXT = false, bool SPLIT = false, bool TREE = false>
 __global__ __launch_bounds__(256) void ssa_fwd_kernel(const FwdParams p)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     if constexpr (DECODE) {
         ssa_fwd_tile<DQK, DV, RB, ALIAS, true, false, false, false>(p, smem);
     } else if constexpr (SPLIT) {
-        ssa_fwd_tile<DQK, DV, RB, ALIAS, false, true, false, true, true>(p, smem);
+        ssa_fwd_tile<DQK, DV, RB, ALIAS, false, true, false, true, true, TREE>(p, smem);
     } else {
-        if (ssa_fwd_tile<DQK, DV, RB, ALIAS, false, false, OUTF32, EXT>(p, smem))
-            ssa_fwd_tile<DQK, DV, RB, ALIAS, false, true, OUTF32, EXT>(p, smem);
+        if (ssa_fwd_tile<DQK, DV, RB, ALIAS, false, false, OUTF32, EXT, false, TREE>(p, smem))
+            ssa_fwd_tile<DQK, DV, RB, ALIAS, false, true, OUTF32, EXT, false, TREE>(p, smem);
     }
 }
 
@@ -1124,11 +1142,11 @@ __global__ __launch_bounds__(256) void ssa_split_add_kernel(const FwdParams p)
     }
 }
 
-template <int DQK, int DV, bool ALIAS, bool OUTF32, bool EXT, bool SPLIT = false>
+template <int DQK, int DV, bool ALIAS, bool OUTF32, bool EXT, bool SPLIT = false, bool TREE = false>
 static hipError_t launch_prefill_kernel(FwdParams p, hipStream_t stream)
 {
     using C = TileCfg<DQK, DV, 4, ALIAS, false>;
-    constexpr auto kern = ssa_fwd_kernel<DQK, DV, 4, ALIAS, false, OUTF32, EXT, SPLIT>;
+    constexpr auto kern = ssa_fwd_kernel<DQK, DV, 4, ALIAS, false, OUTF32, EXT, SPLIT, TREE>;
     hipError_t e = allow_lds<kern>(C::LDS_BYTES);
     if (e != hipSuccess) return e;
     p.rt_begin = 0;
@@ -1160,6 +1178,9 @@ static hipError_t launch_prefill_t(const FwdParams &p, hipStream_t stream)
 template <int DQK, int DV, bool ALIAS>
 static hipError_t launch_extend_t(const FwdParams &p, hipStream_t stream)
 {
+    if (p.tree_masks)
+        return p.n_splits > 1 ? launch_prefill_kernel<DQK, DV, ALIAS, false, true, true, true>(p, stream)
+                              : launch_prefill_kernel<DQK, DV, ALIAS, false, true, false, true>(p, stream);
     if (p.n_splits > 1) return launch_prefill_kernel<DQK, DV, ALIAS, false, true, true>(p, stream);
     return launch_prefill_kernel<DQK, DV, ALIAS, false, true>(p, stream);
 }

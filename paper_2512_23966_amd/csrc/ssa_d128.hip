@@ -28,6 +28,7 @@
 
 #include "ssa_device.h"
 #include "ssa_kernels.h"
+#include "ssa_tree.h"
 
 namespace loza {
 
@@ -59,7 +60,8 @@ struct D128Cfg {
 
 // One pass over one workgroup tile. PRECISE: two-term weights. Returns true (the same in every wave) when the
 // tile has been left unwritten for a PRECISE pass.
-template <bool ALIAS, bool PRECISE, bool OUTF32>
+// TREE: the queries are the nodes of a tree (ssa_tree.h).
+template <bool ALIAS, bool PRECISE, bool OUTF32, bool TREE>
 static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *smem)
 {
     using C = D128Cfg<ALIAS>;
@@ -81,18 +83,25 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     const int64_t Sq = cached ? (int64_t)p.q_len : p.S, pos0 = L - Sq, R = Sq * G, r0 = (int64_t)rt * M;
     const int n_sink = p.n_sink, window = p.window, block = p.block;
     auto last_row = [&](int64_t a, int n) { return a + n - 1 < R ? a + n - 1 : R - 1; };
-    const int i_min = (int)(pos0 + row_position(r0, G)), i_max = (int)(pos0 + row_position(last_row(r0, M), G));
-    if (!PRECISE && i_min < kPrecisePositions) return true;
+    TreeSpan span{};
+    if constexpr (TREE) span = tree_span(p, b);
+    const bool padding = TREE && row_position(r0, G) >= span.nodes;    // (no node among these rows)
+    // (a tree: keys up to i_min are before it, the first window is that of position P, the last that of a chain's end)
+    const int i_min = TREE ? (int)span.P - 1 : (int)(pos0 + row_position(r0, G));
+    const int i_max = TREE ? (padding ? -1 : (int)span.L - 1) : (int)(pos0 + row_position(last_row(r0, M), G));
+    const int i_low = TREE ? (int)span.P : i_min;
+    if (!PRECISE && i_low < kPrecisePositions) return true;
 
     // positions of this wave's rows
     const int64_t w0 = r0 + wave * 32 < R ? r0 + wave * 32 : R - 1;
-    const int wi_min = (int)(pos0 + row_position(w0, G)), wi_max = (int)(pos0 + row_position(last_row(w0, 32), G));
-    const int w_lo_min = window_begin_of(wi_min < 0 ? 0 : wi_min, window, block);
+    const int wi_min = TREE ? i_min : (int)(pos0 + row_position(w0, G)), wi_max = TREE ? i_max : (int)(pos0 + row_position(last_row(w0, 32), G));
+    const int wi_low = TREE ? i_low : wi_min;
+    const int w_lo_min = window_begin_of(wi_low < 0 ? 0 : wi_low, window, block);
     const int w_lo_max = window_begin_of(wi_max < 0 ? 0 : wi_max, window, block);
 
     // ---- live key tiles of 64: sink tiles [0, nA), then window tiles [wt0, wt0 + nB) in rotated order -------
     const int sink_end = i_max < 0 ? 0 : (n_sink < i_max + 1 ? n_sink : i_max + 1);
-    const int win_begin = window_begin_of(i_min < 0 ? 0 : i_min, window, block);
+    const int win_begin = window_begin_of(i_low < 0 ? 0 : i_low, window, block);
     int nA = (sink_end + N - 1) / N;
     const int wt0 = win_begin / N, wt1 = i_max / N;
     int nB;
@@ -163,10 +172,17 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     // ---- the queries: B operands, row ln of each block ------------------------------------------------------
     bf16x8 qf[8];
     int i_row, w_lo_row;
+    TreeRow node{};
     {
         const int64_t row = r0 + wave * 32 + ln, rc = row < R ? row : R - 1, qi = row_position(rc, G);
+        if constexpr (TREE) {
+            node = tree_row(p, span, b, (int)qi);
+            i_row = node.seen ? i_min : kNothing;  // the last key before the tree
+            w_lo_row = node.w_lo;
+        } else {
         i_row = (int)(pos0 + qi);
         w_lo_row = window_begin_of(i_row < 0 ? 0 : i_row, window, block);
+        }
         const uint16_t *qp = p.q + (((int64_t)b * Sq + qi) * p.Hq + (int64_t)g * G + (rc - qi * G)) * D + lh * 8;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) qf[kk] = *(const bf16x8 *)(qp + kk * 16);
@@ -236,10 +252,12 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
         __builtin_amdgcn_s_setprio(0);
         const bool interior = (j0 + 31 <= wi_min) && ((j0 + 31 < n_sink) || (j0 >= w_lo_max));
         if (!interior) {
+            const uint32_t nodes = TREE ? tree_bits(node.mask, j0 + 4 * lh - (int)span.P) : 0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int j = j0 + 4 * lh + 8 * (e >> 2) + (e & 3);
-                const bool ok = (j <= i_row) & ((j < n_sink) | (j >= w_lo_row));
+                bool ok = (j <= i_row) & ((j < n_sink) | (j >= w_lo_row));
+                if constexpr (TREE) ok |= (nodes >> (8 * (e >> 2) + (e & 3))) & 1;
                 s[e] = ok ? s[e] : LOZA_NEG_INF;
             }
         }
@@ -313,6 +331,10 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
         const float l1 = l_run[0] + l_run[1], l = l1 + xor32(l1);
         lse = (m_ref + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
         inv = osum[0] > 0.f ? 1.0f / osum[0] : 0.f;   // a row without a live key gives 0
+        if (TREE && i_row == kNothing) {               // (stages that take no mask have been added to its sums)
+            inv = 0.f;
+            lse = LOZA_NEG_INF;
+        }
         const int row = wave * 32 + ln;
         float mx = 0.f;
         char *op = smem + row * C::OUTROW + lh * 8;
@@ -388,18 +410,18 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     return false;
 }
 
-template <bool ALIAS, bool OUTF32>
+template <bool ALIAS, bool OUTF32, bool TREE>
 __global__ __launch_bounds__(512, 2) void ssa_d128_kernel(const FwdParams p)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    if (ssa_d128_tile<ALIAS, false, OUTF32>(p, smem)) ssa_d128_tile<ALIAS, true, OUTF32>(p, smem);
+    if (ssa_d128_tile<ALIAS, false, OUTF32, TREE>(p, smem)) ssa_d128_tile<ALIAS, true, OUTF32, TREE>(p, smem);
 }
 
-template <bool ALIAS, bool OUTF32>
+template <bool ALIAS, bool OUTF32, bool TREE = false>
 static hipError_t launch_d128_t(FwdParams p, hipStream_t stream)
 {
     using C = D128Cfg<ALIAS>;
-    constexpr auto kern = ssa_d128_kernel<ALIAS, OUTF32>;
+    constexpr auto kern = ssa_d128_kernel<ALIAS, OUTF32, TREE>;
     hipError_t e = allow_lds<kern>(C::LDS_BYTES);
     if (e != hipSuccess) return e;
     const int64_t rows = (p.seqlens ? (int64_t)p.q_len : p.S) * p.G;
@@ -410,6 +432,7 @@ static hipError_t launch_d128_t(FwdParams p, hipStream_t stream)
 
 hipError_t launch_d128_bf16(const FwdParams &p, bool alias, hipStream_t stream)
 {
+    if (p.tree_masks) return alias ? launch_d128_t<true, false, true>(p, stream) : launch_d128_t<false, false, true>(p, stream);
     if (p.out_f32 != nullptr) return alias ? launch_d128_t<true, true>(p, stream) : launch_d128_t<false, true>(p, stream);
     return alias ? launch_d128_t<true, false>(p, stream) : launch_d128_t<false, false>(p, stream);
 }

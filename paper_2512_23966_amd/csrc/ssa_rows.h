@@ -42,6 +42,7 @@
 #include "ssa_device.h"
 #include "ssa_direct.h"
 #include "ssa_kernels.h"
+#include "ssa_tree.h"
 
 namespace loza {
 
@@ -104,9 +105,9 @@ struct RowsCfg {
 };
 
 // One pass: rows M rt .. M rt + M - 1 (M = 16 MB) of (batch b, key head g), tiles `split` of n_splits. EXACT: three-term weights
-// (decode). NT: the key rows are read by this workgroup only. All 256 threads call it together; the LDS it uses
+// (decode). NT: the key rows are read by this workgroup only. TREE: the queries are the nodes of a tree (ssa_tree.h). All 256 threads call it together; the LDS it uses
 // (RowsCfg::LDS_BYTES) must not be in use when it starts.
-template <int DQK, int DV, bool ALIAS, bool NT, bool EXACT, int MB>
+template <int DQK, int DV, bool ALIAS, bool NT, bool EXACT, int MB, bool TREE = false>
 __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, const int b, const int g, const int rt, const int split, const int n_splits)
 {
     using C = RowsCfg<DQK, DV, ALIAS>;
@@ -121,12 +122,17 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
     const int64_t pos0 = L - Sq;
     const int64_t R = Sq * G, r0 = (int64_t)rt * M;
     const int n_sink = p.n_sink, window = p.window, block = p.block;
-    const int i_min = (int)(pos0 + row_position(r0, G));
-    const int i_max = (int)(pos0 + row_position((r0 + M - 1 < R) ? r0 + M - 1 : R - 1, G));
+    TreeSpan span{};
+    if constexpr (TREE) span = tree_span(p, b);
+    const bool padding = TREE && row_position(r0, G) >= span.nodes;    // (no node among these rows)
+    // (a tree: keys up to i_min are before the tree, the first window is that of position P, the last that of a chain's end)
+    const int i_min = TREE ? (int)span.P - 1 : (int)(pos0 + row_position(r0, G));
+    const int i_max = TREE ? (padding ? -1 : (int)span.L - 1) : (int)(pos0 + row_position((r0 + M - 1 < R) ? r0 + M - 1 : R - 1, G));
+    const int i_low = TREE ? (int)span.P : i_min;
 
     // ---- this wave's live key tiles: sink tiles [0, nA), then window tiles [wt0, wt0 + nB), dealt out ---
     const int sink_end = i_max < 0 ? 0 : (n_sink < i_max + 1 ? n_sink : i_max + 1);
-    const int win_begin = window_begin_of(i_min < 0 ? 0 : i_min, window, block);
+    const int win_begin = window_begin_of(i_low < 0 ? 0 : i_low, window, block);
     const int w_lo_max = window_begin_of(i_max < 0 ? 0 : i_max, window, block);
     int nA = (sink_end + N - 1) / N;
     const int wt0 = win_begin / N, wt1 = i_max / N;
@@ -210,13 +216,21 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
     constexpr int KS = DQK / 32;
     bf16x8 qf[MB][KS];
     int i_row[MB], w_lo_row[MB];
+    uint64_t seen[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int64_t row = r0 + mb * 16 + n16, rc = row < R ? row : R - 1;
         const int64_t qi = row_position(rc, G);
         const int hh = (int)(rc - qi * G);
+        if constexpr (TREE) {
+            const TreeRow t = tree_row(p, span, b, (int)qi);
+            i_row[mb] = t.seen ? i_min : kNothing;     // the last key before the tree
+            w_lo_row[mb] = t.w_lo;
+            seen[mb] = t.mask;
+        } else {
         i_row[mb] = (int)(pos0 + qi);
         w_lo_row[mb] = window_begin_of(i_row[mb] < 0 ? 0 : i_row[mb], window, block);
+        }
         const uint16_t *qp = p.q + (((int64_t)b * Sq + qi) * p.Hq + (int64_t)g * G + hh) * DQK + j4 * 8;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk) qf[mb][kk] = *(const bf16x8 *)(qp + kk * 32);
@@ -282,10 +296,12 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
         for (int mb = 0; mb < MB; ++mb) {
             f32x4 s = s2[mb][0] + s2[mb][1];
             if (!interior) {
+                const uint32_t nodes = TREE ? tree_bits(seen[mb], j0 + 4 * j4 - (int)span.P) : 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + 4 * j4 + e;
-                    const bool ok = (j <= i_row[mb]) & ((j < n_sink) | (j >= w_lo_row[mb]));
+                    bool ok = (j <= i_row[mb]) & ((j < n_sink) | (j >= w_lo_row[mb]));
+                    if constexpr (TREE) ok |= (nodes >> e) & 1;
                     s[e] = ok ? s[e] : LOZA_NEG_INF;
                 }
             }
@@ -372,6 +388,10 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
     if (mb > 0) __syncthreads();                   // (the block before has been read)
+    if (TREE && i_row[mb] == kNothing) {           // (tiles that take no mask have been added to its sums)
+        m_ref[mb] = LOZA_NEG_INF;
+        l_run[mb] = 0.f;
+    }
     {
         float l = l_run[mb];
         l += __shfl_xor(l, 16, 64);

@@ -36,6 +36,10 @@ struct TreeRow {
     int w_lo;            // first key of its window
     bool seen;           // false: padding, or a node without a mask: it sees nothing
 };
+// In the place of the last key before the tree for a row that sees nothing. Its scores are masked where tiles are; where a tile takes no mask they
+// are not, and its sums are dropped at the end.
+constexpr int kNothing = -2;
+
 __device__ __forceinline__ TreeRow tree_row(const FwdParams &p, const TreeSpan &s, int b, int r)
 {
     TreeRow t;
@@ -53,6 +57,13 @@ __device__ __forceinline__ TreeRow tree_row(const FwdParams &p, const TreeSpan &
         t.mask = keep;
     }
     return t;
+}
+
+// Bits of nodes first .. first + 31 of a mask, those outside [0, 64) clear. (first > -2^31 + 64)
+__device__ __forceinline__ uint32_t tree_bits(uint64_t mask, int first)
+{
+    const uint64_t up = first < 64 ? mask >> (first & 63) : 0, down = first > -64 ? mask << (-first & 63) : 0;
+    return (uint32_t)(first >= 0 ? up : down);
 }
 
 }  // namespace loza
