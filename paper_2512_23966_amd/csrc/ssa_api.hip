@@ -1297,13 +1297,14 @@ int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t 
 {
     if (!target || !tokens || !parents || !tree_lens || !u_accept || !u_next || !path || !path_lens || !next_token) return LOZA_ERR_NULL;
     loza::VerifyParams p{};
+    p.target = target; p.draft = draft;
     if (int rc = check_verify(p, B, n, V, draft != nullptr)) return rc;
     if (!workspace || workspace_bytes < loza_ssa_verify_tree_workspace_bytes(B, n, V)) return LOZA_ERR_WORKSPACE;
     for (const void *ptr : {(const void *)target, (const void *)draft, (const void *)tokens, (const void *)parents, (const void *)tree_lens,
                             (const void *)u_accept, (const void *)u_next, (const void *)path, (const void *)path_lens, (const void *)next_token})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
-    p.target = target; p.draft = draft; p.tokens = tokens; p.parents = parents; p.tree_lens = tree_lens; p.u_accept = u_accept; p.u_next = u_next;
+    p.tokens = tokens; p.parents = parents; p.tree_lens = tree_lens; p.u_accept = u_accept; p.u_next = u_next;
     p.path = path; p.path_lens = path_lens; p.next_token = next_token; p.partial = (double *)workspace;
     return loza::launch_verify_tree(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }

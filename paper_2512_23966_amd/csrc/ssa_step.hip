@@ -18,6 +18,19 @@ __device__ __forceinline__ T wave_sum(T x)
     return x;
 }
 
+// Sum over this lane and those before it
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const T up = __shfl_up(x, d, 64);
+        if (lane >= d) x += up;
+    }
+    return x;
+}
+
 // ---- tables ------------------------------------------------------------------------------------------
 
 // What request b asks for: pages it holds already, and new ones (0 where its lengths are not possible).
@@ -106,27 +119,17 @@ __global__ __launch_bounds__(256) void step_tables_kernel(const TablesParams p)
             p.slots[at + r] = there ? slot_of(first + r) : -1;
         }
     }
-    if (b == 0 && blockIdx.y == 0) {
-        // what is left: the largest sum of needs that the free list covers is taken
-        const int per = (p.B + 255) / 256, i0 = tid * per, i1 = i0 + per < p.B ? i0 + per : p.B;
-        __shared__ int64_t s_scan[256];
-        int64_t mine = 0;
-        for (int i = i0; i < i1; ++i) mine += request_of(p, i).need;
-        s_scan[tid] = mine;
-        __syncthreads();
+    if (b == 0 && blockIdx.y == 0 && wave == 3) {
+        // What is left: the largest sum of needs that the free list covers is taken. (One wave, 64 requests at a time.)
         int64_t sum = 0, taken = 0;
-        for (int i = 0; i < tid; ++i) sum += s_scan[i];
-        for (int i = i0; i < i1; ++i) {
-            sum += request_of(p, i).need;
-            if (sum <= count) taken = sum;
+        for (int i0 = 0; i0 < p.B; i0 += 64) {
+            const int64_t incl = sum + wave_scan<int64_t>(i0 + lane < p.B ? request_of(p, i0 + lane).need : (int64_t)0);
+            sum = __shfl(incl, 63, 64);
+            const uint64_t covered = __ballot(incl <= count);      // (sums do not fall: the first lanes)
+            if (covered) taken = __shfl(incl, 63 - __builtin_clzll(covered), 64);
+            if (~covered) break;
         }
-        __syncthreads();
-        s_scan[tid] = taken;
-        __syncthreads();
-        if (tid == 0) {
-            for (int i = 1; i < 256; ++i) taken = s_scan[i] > taken ? s_scan[i] : taken;
-            p.free_left[0] = (int32_t)(count - taken);
-        }
+        if (lane == 0) p.free_left[0] = (int32_t)(count - taken);
     }
 }
 
@@ -159,17 +162,20 @@ struct Walk {
 __device__ __forceinline__ void walk_start(Walk &w, const VerifyParams &v, int b)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)b * v.n + lane;
-    int nodes = v.tree_lens[b];
+    const int64_t at = (int64_t)b * v.n + (lane < v.n ? lane : 0);
+    const int nodes = v.tree_lens[b];
+    w.parent = v.parents[at];
+    w.token = v.tokens[at];
+    w.u = v.u_accept[at];
     w.nodes = nodes < 0 ? 0 : nodes < v.n ? nodes : v.n;
-    const bool there = lane > 0 && lane < w.nodes;
-    w.parent = there ? v.parents[at] : -1;
-    w.token = there ? v.tokens[at] : -1;
-    if (w.parent < 0 || w.parent >= lane || w.token < 0 || w.token >= v.V) w.parent = -1;   // nobody's child
-    const int64_t row = ((int64_t)b * v.n + (w.parent < 0 ? 0 : w.parent)) * v.V + (w.parent < 0 ? 0 : w.token);
-    w.p = w.parent < 0 ? 0.f : v.target[row];
-    w.q = w.parent < 0 ? 0.f : v.draft ? v.draft[row] : 1.f;
-    w.u = w.parent < 0 ? 0.f : v.u_accept[at];
+    if (lane == 0 || lane >= w.nodes || w.parent < 0 || w.parent >= lane || w.token < 0 || w.token >= v.V) {
+        w.parent = w.token = -1;                   // nobody's child
+        w.p = w.q = 0.f;
+    } else {
+        const int64_t row = ((int64_t)b * v.n + w.parent) * v.V + w.token;
+        w.p = v.target[row];
+        w.q = v.draft ? v.draft[row] : 1.f;
+    }
     w.cur = 0;
     w.last = 0;
     w.c = 0;
@@ -238,26 +244,37 @@ struct Residual {
         token = w.token;
         gone = DRAFT ? 0 : w.gone & __ballot(token >= x0 && token < x1);
     }
-    __device__ __forceinline__ double at(int x) const
+    __device__ __forceinline__ double weight(int x, float px, float qx) const
     {
         if constexpr (DRAFT) {
-            const double a = (double)p[x] - c * (double)q[x];
+            const double a = (double)px - c * (double)qx;
             return a > 0 ? a : 0;
         } else {
-            float a = p[x];
-            for (uint64_t g = gone; g; g &= g - 1) a = x == lane_value(token, __builtin_ctzll(g)) ? 0.f : a;
-            return a;
+            for (uint64_t g = gone; g; g &= g - 1) px = x == lane_value(token, __builtin_ctzll(g)) ? 0.f : px;
+            return px;
         }
     }
+    __device__ __forceinline__ double at(int x) const { return weight(x, p[x], DRAFT ? q[x] : 0.f); }
 };
 
-// This wave's share (tokens x0 + first, x0 + first + step, .. below x1) of the sum over a slice, in every lane
+// This wave's share of the sum over a slice, in every lane: 4 tokens a lane at a time (rows of a multiple of 4 tokens: 16-byte loads),
+// the first ones at x0 + 4 first, the next 4 step further.
 template <bool DRAFT>
-__device__ __forceinline__ double wave_residual(const Residual<DRAFT> &r, int x0, int x1, int first, int step)
+__device__ __forceinline__ double wave_residual(const Residual<DRAFT> &r, bool quads, int x0, int x1, int first, int step)
 {
     double sum = 0;
+    if (quads) {
 #pragma unroll 4
-    for (int x = x0 + first; x < x1; x += step) sum += r.at(x);
+        for (int x = x0 + 4 * first; x < x1; x += 4 * step) {
+            const float4 p = *(const float4 *)(r.p + x);
+            float4 q = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (DRAFT) q = *(const float4 *)(r.q + x);
+            sum += (r.weight(x, p.x, q.x) + r.weight(x + 1, p.y, q.y)) + (r.weight(x + 2, p.z, q.z) + r.weight(x + 3, p.w, q.w));
+        }
+    } else {
+#pragma unroll 4
+        for (int x = x0 + first; x < x1; x += step) sum += r.at(x);
+    }
     return wave_sum(sum);
 }
 
@@ -287,7 +304,7 @@ __global__ __launch_bounds__(256) void verify_sum_kernel(const VerifyParams v, c
     }
     walk_on<DRAFT>(w);
     const int x0 = slice * v.slice_len, x1 = x0 + v.slice_len < v.V ? x0 + v.slice_len : v.V;
-    const double sum = wave_residual<DRAFT>(Residual<DRAFT>(w, v, b, x0, x1), x0, x1, threadIdx.x, 256);
+    const double sum = wave_residual<DRAFT>(Residual<DRAFT>(w, v, b, x0, x1), v.quads, x0, x1, threadIdx.x, 256);
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) part[round * v.slices + slice] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
@@ -311,7 +328,7 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
             __syncthreads();
             for (int s = wave; s < v.slices; s += 16) {
                 const int x0 = s * v.slice_len, x1 = x0 + v.slice_len < v.V ? x0 + v.slice_len : v.V;
-                const double sum = wave_residual<DRAFT>(Residual<DRAFT>(w, v, b, x0, x1), x0, x1, lane, 64);
+                const double sum = wave_residual<DRAFT>(Residual<DRAFT>(w, v, b, x0, x1), v.quads, x0, x1, lane, 64);
                 if (lane == 0) s_part[s] = sum;
             }
             __syncthreads();
@@ -340,9 +357,25 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
         if (w.s > 0) {
             // the slice in which the running sum passes the threshold, then the token (every thread takes a run of tokens)
             double thr = (double)v.u_next[b] * w.s;
-            int slice = 0;
-            double at = 0;
-            for (; slice < v.slices - 1 && !(at + s_part[slice] > thr); ++slice) at += s_part[slice];
+            double four[4], upto = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                four[i] = 4 * lane + i < v.slices ? s_part[4 * lane + i] : 0;
+                upto += four[i];
+            }
+            upto = wave_scan(upto);
+            const uint64_t beyond = __ballot(upto > thr);
+            const int l = beyond ? __builtin_ctzll(beyond) : (v.slices - 1) / 4;
+            double at = l > 0 ? __shfl(upto, l > 0 ? l - 1 : 0, 64) : 0;
+            int slice = 4 * l;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const double part_i = __shfl(four[i], l, 64);
+                if (slice == 4 * l + i && slice < v.slices - 1 && !(at + part_i > thr)) {
+                    at += part_i;
+                    ++slice;
+                }
+            }
             thr -= at;
             const int x0 = slice * v.slice_len, x1 = x0 + v.slice_len < v.V ? x0 + v.slice_len : v.V;
             const int per = (v.slice_len + 1023) / 1024;
@@ -350,12 +383,7 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
             int a = x0 + tid * per, e = a + per < x1 ? a + per : x1;
             double mine = 0;
             for (int x = a; x < e; ++x) mine += res.at(x);
-            double incl = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double up = __shfl_up(incl, d, 64);
-                if (lane >= d) incl += up;
-            }
+            const double incl = wave_scan(mine);
             if (lane == 63) s_wave[wave] = incl;
             if (tid == 0) s_first = 1023;
             __syncthreads();
@@ -449,7 +477,8 @@ void verify_plan(VerifyParams &p, bool draft)
     if (slices > ((int64_t)p.V + 1023) / 1024) slices = ((int64_t)p.V + 1023) / 1024;
     p.slice_len = (int)(((p.V + slices - 1) / slices + 63) / 64 * 64);
     p.slices = (p.V + p.slice_len - 1) / p.slice_len;
-    p.rounds = draft ? 2 : 1;
+    p.rounds = draft ? (p.n < 4 ? p.n : 4) : 1;
+    p.quads = p.V % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.target) | reinterpret_cast<uintptr_t>(p.draft)) & 15u) == 0;
 }
 
 template <bool DRAFT>
