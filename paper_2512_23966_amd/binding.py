@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from pathlib import Path
 
@@ -677,16 +678,40 @@ def loza_ssa_backward_blocks(q, k, v, out, lse, dout, dq, dk, dv, sink_blocks, l
 LOZA_TREE_MAX_NODES = 64
 
 
-def _dev_ptr_or_none(t, dtype, name):
-    return None if t is None else _dev_ptr(t, dtype, name)
+def _launch_device(t) -> int:
+    """The current device, to which a launch goes (-2, which no tensor is on, where `t` is not on a GPU)."""
+    return torch._C._cuda_getDevice() if isinstance(t, torch.Tensor) and t.is_cuda else -2
 
 
-def _call(fn_name, tensors, *args) -> None:
-    """The launch goes to the current device: every tensor has to be there."""
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"{fn_name}: a tensor is on device {t.get_device()}, the current one is {here}")
+def _ptr(t, dtype, shape, name: str, device: int):
+    """Address of a contiguous tensor of that type and shape (None: any) on that device; None for None. (One test of everything first: a
+    dozen tensors looked at one property at a time are half the host's time of a call.)"""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and (shape is None or t.shape == shape) and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _dev_ptr(t, dtype, name)
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    raise ValueError(f"{name} is on device {t.get_device()}, the current one is {device}")
+
+
+def _heads(t, dtype, shape, name: str, device: int):
+    """(pointer, token stride, head stride) of a [T, H, d] tensor whose columns lie side by side; zeros for None."""
+    if t is None:
+        return None, 0, 0
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        st, sh, sc = t.stride()
+        if sc == 1 or shape[2] == 1:
+            return t.data_ptr(), st, sh
+        raise ValueError(f"the columns of {name} must lie side by side")
+    _dev_ptr(t.contiguous() if isinstance(t, torch.Tensor) else t, dtype, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    raise ValueError(f"{name} is on device {t.get_device()}, the current one is {device}")
+
+
+def _call(fn_name, *args) -> None:
     rc = getattr(lib(), fn_name)(*args)
     if rc != LOZA_OK:
         raise LozaError(rc, fn_name)
@@ -697,52 +722,33 @@ def loza_ssa_step_tables(cache_lens, new_lens, parents, free_pages, free_count, 
     """Block table entries, slots, positions and (``parents`` given: the tokens are trees) ancestor masks of a step. cache_lens, new_lens,
     granted, seqlens [B], parents (or None), positions, slots [B,n], block_table [B,max_pages], free_pages [F], free_count and
     free_left [1], all int32 on the GPU; masks [B,n] int64 (None without parents). ``block_table`` is extended in place."""
+    dev, i32 = _launch_device(positions), torch.int32
     B, n = positions.shape
-    i32 = torch.int32
-    if any(t.shape != (B,) for t in (cache_lens, new_lens, granted, seqlens)) or slots.shape != (B, n) or free_count.numel() != 1 \
-            or free_left.numel() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError("shape mismatch between the lengths, block_table, free_pages, positions, slots")
-    if (parents is None) != (masks is None) or (parents is not None and (parents.shape != (B, n) or masks.shape != (B, n))):
+    rows, both, (num_free,), most = (B,), (B, n), free_pages.shape, block_table.shape[-1]
+    if (parents is None) != (masks is None):
         raise ValueError("parents and masks must both be [B, n], or both None")
-    _call("loza_ssa_step_tables", (cache_lens, new_lens, parents, free_pages, free_count, block_table, granted, seqlens, positions, slots, masks, free_left),
-        _dev_ptr(cache_lens, i32, "cache_lens"), _dev_ptr(new_lens, i32, "new_lens"), _dev_ptr_or_none(parents, i32, "parents"),
-        _dev_ptr(free_pages, i32, "free_pages"), _dev_ptr(free_count, i32, "free_count"), _dev_ptr(block_table, i32, "block_table"),
-        B, n, free_pages.shape[0], int(num_pages), int(page_size), block_table.shape[1], _dev_ptr(granted, i32, "granted"),
-        _dev_ptr(seqlens, i32, "seqlens"), _dev_ptr(positions, i32, "positions"), _dev_ptr(slots, i32, "slots"),
-        _dev_ptr_or_none(masks, torch.int64, "masks"), _dev_ptr(free_left, i32, "free_left"), _stream(stream))
+    _call("loza_ssa_step_tables", _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(new_lens, i32, rows, "new_lens", dev),
+          _ptr(parents, i32, both, "parents", dev), _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev),
+          _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, num_pages, page_size, most,
+          _ptr(granted, i32, rows, "granted", dev), _ptr(seqlens, i32, rows, "seqlens", dev), _ptr(positions, i32, both, "positions", dev),
+          _ptr(slots, i32, both, "slots", dev), _ptr(masks, torch.int64, both, "masks", dev), _ptr(free_left, i32, (1,), "free_left", dev), _stream(stream))
 
 
 def loza_ssa_rope_frequencies(rot_dim, base, factor=1.0, original_context=0, slow_turns=1.0, fast_turns=32.0):
     """(freq, mscale): float64 CPU tensor [rot_dim / 2] of radians per position, and the scale of queries and keys. Host only."""
     freq, m = torch.empty(max(0, int(rot_dim)) // 2 or 1, dtype=torch.float64), ctypes.c_float()
-    rc = lib().loza_ssa_rope_frequencies(int(rot_dim), float(base), float(factor), int(original_context), float(slow_turns), float(fast_turns),
-                                         ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(m))
-    if rc != LOZA_OK:
-        raise LozaError(rc, "loza_ssa_rope_frequencies")
+    _call("loza_ssa_rope_frequencies", int(rot_dim), float(base), float(factor), int(original_context), float(slow_turns), float(fast_turns),
+          ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(m))
     return freq, m.value
 
 
-def _heads(t: torch.Tensor, dtype, name: str):
-    """(pointer, token stride, head stride) of a [T, H, d] tensor whose columns lie side by side."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a tensor on the GPU")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [T, H, d]")
-    if t.shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"the columns of {name} must lie side by side")
-    return t.data_ptr(), t.stride(0), t.stride(1)
-
-
 def _rope(fn_name, dtype, x, positions, freq, out, rot_begin, interleaved, mscale, inverse, stream):
-    xp, xt, xh = _heads(x, dtype, "x")
-    op, ot, oh = _heads(out, dtype, "out")
-    T, H, d = x.shape
-    if out.shape != x.shape or positions.shape != (T,) or freq.dim() != 1:
-        raise ValueError("shape mismatch between x, out, positions, freq")
-    _call(fn_name, (x, positions, freq, out), xp, _dev_ptr(positions, torch.int32, "positions"), _dev_ptr(freq, torch.float64, "freq"), op, T, H, d, xt, xh, ot, oh,
-                                 int(rot_begin), 2 * freq.shape[0], int(bool(interleaved)), int(bool(inverse)), float(mscale), _stream(stream))
+    dev, shape, (pairs,) = _launch_device(x), x.shape, freq.shape
+    T, H, d = shape
+    xp, xt, xh = _heads(x, dtype, shape, "x", dev)
+    op, ot, oh = _heads(out, dtype, shape, "out", dev)
+    _call(fn_name, xp, _ptr(positions, torch.int32, (T,), "positions", dev), _ptr(freq, torch.float64, None, "freq", dev), op, T, H, d, xt, xh, ot, oh,
+          rot_begin, 2 * pairs, bool(interleaved), bool(inverse), mscale, _stream(stream))
 
 
 def loza_ssa_rope(x, positions, freq, out, rot_begin, interleaved, mscale=1.0, inverse=False, stream=None):
@@ -758,29 +764,26 @@ def loza_ssa_rope_f32(x, positions, freq, out, rot_begin, interleaved, mscale=1.
 
 
 def _rope_append(fn_name, dtype, q, k, v, positions, slots, freq, q_out, k_rows, v_rows, q_rot_begin, k_rot_begin, interleaved, mscale, stream):
+    dev, i32, (pairs,) = _launch_device(k), torch.int32, freq.shape
     T, Hkv, d_k = k.shape
-    if positions.shape != (T,) or slots.shape != (T,) or freq.dim() != 1:
-        raise ValueError("positions and slots must be [T], freq [rot_dim / 2]")
-    if (q is None) != (q_out is None) or (q is not None and (q_out.shape != q.shape or q.shape[0] != T)):
-        raise ValueError("q and q_out must both be [T, Hq, d_q], or both None")
-    if k_rows.dim() < 3 or k_rows.shape[-2:] != (Hkv, d_k):
+    *lead, hk, dk = k_rows.shape
+    if not lead or (hk, dk) != (Hkv, d_k):
         raise ValueError("k_rows must be [..., Hkv, d_k]")
-    if (v is None) != (v_rows is None):
-        raise ValueError("v and v_rows go together")
-    rows, d_v = k_rows[..., 0, 0].numel(), 0
+    if (q is None) != (q_out is None) or (v is None) != (v_rows is None):
+        raise ValueError("q and q_out go together, and so do v and v_rows")
+    rows, Hq, d_q, d_v = math.prod(lead), 0, 0, 0
+    if q is not None:
+        _, Hq, d_q = q.shape
     if v is not None:
         d_v = v.shape[-1]
-        if v.shape != (T, Hkv, d_v) or v_rows.shape != (*k_rows.shape[:-1], d_v):
-            raise ValueError("v must be [T, Hkv, d_v], v_rows [..., Hkv, d_v] with the rows of k_rows")
-    qp, qt, qh = _heads(q, dtype, "q") if q is not None else (None, 0, 0)
-    op, ot, oh = _heads(q_out, dtype, "q_out") if q is not None else (None, 0, 0)
-    kp, kt, kh = _heads(k, dtype, "k")
-    vp, vt, vh = _heads(v, dtype, "v") if v is not None else (None, 0, 0)
-    Hq, d_q = q.shape[1:] if q is not None else (0, 0)
-    _call(fn_name, (q, k, v, positions, slots, freq, q_out, k_rows, v_rows), qp, kp, vp, _dev_ptr(positions, torch.int32, "positions"), _dev_ptr(slots, torch.int32, "slots"),
-                                 _dev_ptr(freq, torch.float64, "freq"), op, _dev_ptr(k_rows, dtype, "k_rows"), _dev_ptr_or_none(v_rows, dtype, "v_rows"),
-                                 T, Hq, Hkv, d_q, d_k, d_v, qt, qh, ot, oh, kt, kh, vt, vh, rows, int(q_rot_begin), int(k_rot_begin),
-                                 2 * freq.shape[0], int(bool(interleaved)), float(mscale), _stream(stream))
+    qp, qt, qh = _heads(q, dtype, (T, Hq, d_q), "q", dev)
+    op, ot, oh = _heads(q_out, dtype, (T, Hq, d_q), "q_out", dev)
+    kp, kt, kh = _heads(k, dtype, (T, Hkv, d_k), "k", dev)
+    vp, vt, vh = _heads(v, dtype, (T, Hkv, d_v), "v", dev)
+    _call(fn_name, qp, kp, vp, _ptr(positions, i32, (T,), "positions", dev), _ptr(slots, i32, (T,), "slots", dev),
+          _ptr(freq, torch.float64, None, "freq", dev), op, _ptr(k_rows, dtype, None, "k_rows", dev),
+          _ptr(v_rows, dtype, (*lead, Hkv, d_v), "v_rows", dev), T, Hq, Hkv, d_q, d_k, d_v, qt, qh, ot, oh, kt, kh, vt, vh, rows,
+          q_rot_begin, k_rot_begin, 2 * pairs, bool(interleaved), mscale, _stream(stream))
 
 
 def loza_ssa_rope_append(q, k, v, positions, slots, freq, q_out, k_rows, v_rows, q_rot_begin, k_rot_begin, interleaved, mscale=1.0, stream=None):
@@ -809,30 +812,24 @@ def loza_ssa_extend_tree(q, kcache, vcache, seqlens, tree_lens, masks, out, lse,
     """Attention of a tree of drafted tokens per sequence over a cache that holds their rows. q [B,n,Hq,d_qk], out [B,n,Hq,d_v] bf16, lse [B,Hq,n]
     fp32; kcache, vcache as for :func:`loza_ssa_extend`, or pages with ``block_table`` [B,max_pages]; seqlens (the nodes' rows included), tree_lens [B]
     int32, masks [B,n] int64 as :func:`loza_ssa_step_tables` makes them. block = 1: the pattern in tokens. workspace: as for the extends."""
+    dev, bf, i32 = _launch_device(q), torch.bfloat16, torch.int32
     B, n, Hq, d_qk = q.shape
-    lead, size, Hkv, _ = kcache.shape
-    d_v = out.shape[3]
-    if kcache.shape[3] != d_qk or out.shape != (B, n, Hq, d_v) or lse.shape != (B, Hq, n) or seqlens.shape != (B,) or tree_lens.shape != (B,) \
-            or masks.shape != (B, n):
-        raise ValueError("shape mismatch between q, kcache, seqlens, tree_lens, masks, out, lse")
-    if block_table is None and lead != B or block_table is not None and (block_table.dim() != 2 or block_table.shape[0] != B):
-        raise ValueError("kcache must be [B, S_max, Hkv, d_qk], or pages with a block_table [B, max_pages]")
-    if vcache is not kcache and vcache.shape != (lead, size, Hkv, d_v):
-        raise ValueError("vcache must have the rows of kcache (or be the very tensor passed as kcache)")
-    bf, i32 = torch.bfloat16, torch.int32
-    qp, kp = _dev_ptr(q, bf, "q"), _dev_ptr(kcache, bf, "kcache")
-    vp = kp if vcache is kcache else _dev_ptr(vcache, bf, "vcache")
-    paging = (lead, size, block_table.shape[1]) if block_table is not None else (0, 0, 0)
-    S_max = paging[1] * paging[2] if block_table is not None else size
-    pattern = (int(sink_blocks), _win(local_blocks), int(block))
-    need = loza_ssa_extend_tree_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, *pattern)
-    if need and workspace is None:
-        workspace = _scratch(need, stream)
-    wp, wn = (None, 0) if workspace is None else (_dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel())
-    _call("loza_ssa_extend_tree", (q, kcache, vcache, block_table, seqlens, tree_lens, masks, out, lse, workspace), qp, kp, vp, _dev_ptr_or_none(block_table, i32, "block_table"), _dev_ptr(seqlens, i32, "seqlens"),
-                                    _dev_ptr(tree_lens, i32, "tree_lens"), _dev_ptr(masks, torch.int64, "masks"), _dev_ptr(out, bf, "out"),
-                                    _dev_ptr(lse, torch.float32, "lse"), B, Hq, Hkv, S_max, *paging, n, d_qk, d_v, *pattern, float(scale),
-                                    wp, wn, _stream(stream))
+    lead, size, Hkv, d_k = kcache.shape
+    d_v = out.shape[-1]
+    if d_k != d_qk or (block_table is None and lead != B):
+        raise ValueError("kcache must be [B, S_max, Hkv, d_qk], or pages [num_pages, page_size, Hkv, d_qk] with a block_table")
+    paging = (0, 0, 0) if block_table is None else (lead, size, block_table.shape[-1])
+    S_max = size if block_table is None else size * paging[2]
+    pattern = (sink_blocks, _win(local_blocks), block)
+    kp = _ptr(kcache, bf, None, "kcache", dev)
+    args = (_ptr(q, bf, None, "q", dev), kp, kp if vcache is kcache else _ptr(vcache, bf, (lead, size, Hkv, d_v), "vcache", dev),
+            _ptr(block_table, i32, (B, paging[2]), "block_table", dev), _ptr(seqlens, i32, (B,), "seqlens", dev), _ptr(tree_lens, i32, (B,), "tree_lens", dev),
+            _ptr(masks, torch.int64, (B, n), "masks", dev), _ptr(out, bf, (B, n, Hq, d_v), "out", dev), _ptr(lse, torch.float32, (B, Hq, n), "lse", dev))
+    if workspace is None:
+        need = loza_ssa_extend_tree_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, *pattern)
+        workspace = _scratch(need, stream) if need else None
+    _call("loza_ssa_extend_tree", *args, B, Hq, Hkv, S_max, *paging, n, d_qk, d_v, *pattern, scale,
+          _ptr(workspace, torch.uint8, None, "workspace", dev), 0 if workspace is None else workspace.numel(), _stream(stream))
 
 
 def loza_ssa_verify_tree_workspace_bytes(B, n, V) -> int:
@@ -842,29 +839,24 @@ def loza_ssa_verify_tree_workspace_bytes(B, n, V) -> int:
 def loza_ssa_verify_tree(target, draft, tokens, parents, tree_lens, u_accept, u_next, path, path_lens, next_token, workspace, stream=None):
     """Which drafted nodes hold, and the token after them. target [B,n,V] float32 probabilities, draft likewise or None (drafts that are not random),
     tokens, parents, path [B,n], tree_lens, path_lens, next_token [B] int32, u_accept [B,n], u_next [B] float32, workspace uint8."""
+    dev, f32, i32 = _launch_device(target), torch.float32, torch.int32
     B, n, V = target.shape
-    f32, i32 = torch.float32, torch.int32
-    if (draft is not None and draft.shape != target.shape) or any(t.shape != (B, n) for t in (tokens, parents, u_accept, path)) \
-            or any(t.shape != (B,) for t in (tree_lens, u_next, path_lens, next_token)):
-        raise ValueError("shape mismatch between target, draft, tokens, parents, tree_lens, u_accept, u_next, path, path_lens, next_token")
-    _call("loza_ssa_verify_tree", (target, draft, tokens, parents, tree_lens, u_accept, u_next, path, path_lens, next_token, workspace), _dev_ptr(target, f32, "target"), _dev_ptr_or_none(draft, f32, "draft"), _dev_ptr(tokens, i32, "tokens"),
-                                    _dev_ptr(parents, i32, "parents"), _dev_ptr(tree_lens, i32, "tree_lens"), _dev_ptr(u_accept, f32, "u_accept"),
-                                    _dev_ptr(u_next, f32, "u_next"), _dev_ptr(path, i32, "path"), _dev_ptr(path_lens, i32, "path_lens"),
-                                    _dev_ptr(next_token, i32, "next_token"), B, n, V, _dev_ptr(workspace, torch.uint8, "workspace"),
-                                    workspace.numel(), _stream(stream))
+    rows, both = (B,), (B, n)
+    _call("loza_ssa_verify_tree", _ptr(target, f32, None, "target", dev), _ptr(draft, f32, (B, n, V), "draft", dev), _ptr(tokens, i32, both, "tokens", dev),
+          _ptr(parents, i32, both, "parents", dev), _ptr(tree_lens, i32, rows, "tree_lens", dev), _ptr(u_accept, f32, both, "u_accept", dev),
+          _ptr(u_next, f32, rows, "u_next", dev), _ptr(path, i32, both, "path", dev), _ptr(path_lens, i32, rows, "path_lens", dev),
+          _ptr(next_token, i32, rows, "next_token", dev), B, n, V, _ptr(workspace, torch.uint8, None, "workspace", dev), workspace.numel(), _stream(stream))
 
 
 def loza_ssa_keep_accepted(k_rows, v_rows, slots, path, path_lens, stream=None):
     """Moves the rows of the accepted path: row slots[b, path[b, i]] of the cache becomes row slots[b, i]. k_rows [layers, ..., Hkv, d]: caches of one
     or more layers, any type, at least 4 dimensions, the first of them the layers, the last two a row; v_rows likewise or None."""
+    dev, i32 = _launch_device(k_rows), torch.int32
     B, n = slots.shape
-    i32 = torch.int32
-    if path.shape != (B, n) or path_lens.shape != (B,):
-        raise ValueError("shape mismatch between slots, path, path_lens")
-    if k_rows.dim() < 4 or (v_rows is not None and v_rows.shape[:-2] != k_rows.shape[:-2]):
+    layers, *lead, hk, dk = k_rows.shape
+    if not lead or (v_rows is not None and v_rows.shape[:-2] != k_rows.shape[:-2]):
         raise ValueError("k_rows must be [layers, ..., Hkv, d], v_rows of the same layers and rows")
-    layers, rows = k_rows.shape[0], k_rows[0, ..., 0, 0].numel()
-    row_bytes = [0 if t is None else t.shape[-2] * t.shape[-1] * t.element_size() for t in (k_rows, v_rows)]
-    _call("loza_ssa_keep_accepted", (k_rows, v_rows, slots, path, path_lens), _dev_ptr(k_rows, k_rows.dtype, "k_rows"), None if v_rows is None else _dev_ptr(v_rows, v_rows.dtype, "v_rows"),
-                                      _dev_ptr(slots, i32, "slots"), _dev_ptr(path, i32, "path"), _dev_ptr(path_lens, i32, "path_lens"), B, n, layers,
-                                      rows, *row_bytes, _stream(stream))
+    v_bytes = 0 if v_rows is None else v_rows.shape[-2] * v_rows.shape[-1] * v_rows.element_size()
+    _call("loza_ssa_keep_accepted", _ptr(k_rows, k_rows.dtype, None, "k_rows", dev), None if v_rows is None else _ptr(v_rows, v_rows.dtype, None, "v_rows", dev),
+          _ptr(slots, i32, None, "slots", dev), _ptr(path, i32, (B, n), "path", dev), _ptr(path_lens, i32, (B,), "path_lens", dev), B, n, layers,
+          math.prod(lead), hk * dk * k_rows.element_size(), v_bytes, _stream(stream))
