@@ -549,6 +549,11 @@ int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int3
 size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
                                             int64_t sink_blocks, int64_t local_blocks, int64_t block);
 
+/* Host-only (ours), for tests and tools: the loza_kernel that a tree call of these sizes runs with scratch memory (scratch != 0) or without;
+ * *n_splits (may be NULL): the workgroups that share the keys of a row. Negative on sizes that the call refuses. */
+int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int64_t sink_blocks, int64_t local_blocks,
+                                int64_t block, int scratch, int *n_splits);
+
 /*
  * Which drafts hold, and the token after them, from given random numbers, such that tokens are distributed as the target's
  * (recursive rejection sampling).

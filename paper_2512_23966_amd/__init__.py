@@ -22,6 +22,6 @@ from .binding import (  # noqa: F401
     loza_ssa_decode_static, LOZA_DECODE_STATIC_BYTES,
     loza_ssa_forward_kernel, loza_ssa_decode_kernel, loza_ssa_backward_split, KERNEL_TILES, KERNEL_ROWS, KERNEL_D128,
     loza_ssa_step_tables, loza_ssa_rope, loza_ssa_rope_f32, loza_ssa_rope_append, loza_ssa_rope_append_f32, loza_ssa_rope_frequencies,
-    loza_ssa_extend_tree, loza_ssa_extend_tree_workspace_bytes, loza_ssa_verify_tree, loza_ssa_verify_tree_workspace_bytes,
+    loza_ssa_extend_tree, loza_ssa_extend_tree_workspace_bytes, loza_ssa_extend_tree_kernel, loza_ssa_verify_tree, loza_ssa_verify_tree_workspace_bytes,
     loza_ssa_keep_accepted, LOZA_TREE_MAX_NODES,
 )

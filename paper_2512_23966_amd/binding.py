@@ -41,6 +41,7 @@ EXPORTS = (
     "loza_ssa_forward_kernel", "loza_ssa_decode_kernel", "loza_ssa_backward_split",
     "loza_ssa_step_tables", "loza_ssa_rope", "loza_ssa_rope_f32", "loza_ssa_rope_append", "loza_ssa_rope_append_f32",
     "loza_ssa_rope_frequencies", "loza_ssa_extend_tree", "loza_ssa_extend_tree_workspace_bytes",
+    "loza_ssa_extend_tree_kernel",
     "loza_ssa_verify_tree", "loza_ssa_verify_tree_workspace_bytes", "loza_ssa_keep_accepted",
 )
 KERNEL_TILES, KERNEL_ROWS, KERNEL_D128 = 1, 2, 3
@@ -149,6 +150,8 @@ def lib() -> ctypes.CDLL:
         L.loza_ssa_extend_tree.argtypes = [vp] * 9 + [ci, ci, ci, i64, i64, ci, ci, ci, ci, ci, i64, i64, i64, f32, vp, sz, vp]
         L.loza_ssa_extend_tree_workspace_bytes.restype = sz
         L.loza_ssa_extend_tree_workspace_bytes.argtypes = [ci, ci, ci, i64, ci, ci, ci, i64, i64, i64]
+        L.loza_ssa_extend_tree_kernel.restype = ci
+        L.loza_ssa_extend_tree_kernel.argtypes = [ci, ci, ci, i64, ci, ci, i64, i64, i64, ci, ctypes.POINTER(ci)]
         L.loza_ssa_verify_tree.restype = ci
         L.loza_ssa_verify_tree.argtypes = [vp] * 10 + [ci, ci, ci, vp, sz, vp]
         L.loza_ssa_verify_tree_workspace_bytes.restype = sz
@@ -805,6 +808,13 @@ def loza_ssa_extend_tree_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, sink, 
     """Bytes of scratch memory with which :func:`loza_ssa_extend_tree` lets several workgroups share the keys of a query (0: it has no use
     for any). Host only."""
     return int(lib().loza_ssa_extend_tree_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, sink, _win(local), block))
+
+
+def loza_ssa_extend_tree_kernel(B, Hq, Hkv, S_max, n, d_qk, sink, local, block=1, scratch=True):
+    """(KERNEL_..., workgroups that share the keys of a row) of a tree call of these sizes. Host only."""
+    k = ctypes.c_int()
+    kernel = lib().loza_ssa_extend_tree_kernel(B, Hq, Hkv, int(S_max), n, d_qk, int(sink), _win(local), int(block), int(bool(scratch)), ctypes.byref(k))
+    return _checked(kernel, "loza_ssa_extend_tree_kernel"), k.value
 
 
 def loza_ssa_extend_tree(q, kcache, vcache, seqlens, tree_lens, masks, out, lse, sink_blocks, local_blocks, block, scale,

@@ -216,6 +216,58 @@ ExtendPlan extend_plan(int B, int Hkv, int G, int64_t q_len, int64_t S, int d_qk
     return best;
 }
 
+// Which kernel takes a tree of drafted tokens, how many workgroups share the keys of a row (1 without scratch memory), and whether tiles that are
+// not split take two-term weights from the outset. A time model in microseconds, like extend_plan's, fitted to 250 sizes of 1 to 16 sequences and
+// 2 to 64 nodes; a tree has at most 64 nodes, so most calls leave the chip idle unless keys are shared, and calls that the few-rows kernel
+// takes in one full round are not left to it (window 8192, wide: one sequence of 33 nodes 153 us, its tiles in 15 parts 78; 8 of 8 nodes 156, in 8 113).
+// Width 128 has the few-rows kernel and tiles of 256 rows, split or not; a tile that is mostly padding costs less (8 key heads, window 4096,
+// 8 sequences of 37 nodes: 128-row tiles in 4 parts 88 us, 256-row tiles in 4 parts 52).
+// The wide shape has the few-rows kernel and tiles of 128 rows. Where these are not split, one with a large result is computed again
+// with two-term weights behind all others, which costs more than two-term weights throughout as long as there are at most two rounds of tiles; whether
+// there is one is a matter of values: of random ones, some tile in 80 has one at 1,024 live keys (8 sequences of 48 nodes, 1 + 7 blocks: 143 us,
+// two terms throughout 88), none in 512 at 8,320 (64 nodes: 421, two terms 580). The line is drawn at 2,304 live keys.
+struct TreePlan {
+    loza_kernel kernel;
+    int n_splits;
+    bool precise;
+};
+
+TreePlan tree_plan(int B, int Hkv, int G, int64_t n, int64_t S, int d_qk, const Pattern &pat, bool scratch)
+{
+    const bool wide = d_qk > 128;
+    const int64_t rows = n * G, heads = (int64_t)B * Hkv, groups = (rows + 15) / 16 * heads;
+    int64_t live = (int64_t)pat.n_sink + (int64_t)pat.window * pat.block;
+    if (live > S) live = S;
+    const double keys = (double)live, all = (double)(rows * heads);
+    auto rounds = [](int64_t workgroups) { return (double)((workgroups + kComputeUnits - 1) / kComputeUnits); };
+    TreePlan best{LOZA_KERNEL_ROWS, 1, false};
+    double t = 1e30;
+    auto offer = [&](loza_kernel kernel, int64_t k, bool precise, double t_k) { if (t_k < t) { t = t_k; best = TreePlan{kernel, (int)k, precise}; } };
+    const int64_t most = scratch ? kMaxSplits : 1;
+    if (loza::few_rows_bf16(B, Hkv, rows)) {
+        const bool pairs = !wide && groups > kComputeUnits && (rows + 31) / 32 * heads <= kComputeUnits;
+        for (int64_t k = 1; k <= most && (k == 1 || groups * k <= kComputeUnits); ++k) {
+            const double steps = ceil((keys / 16 + 2) / (4.0 * k)), merge = k == 1 ? 0 : wide ? 2.5 + all * (2.8e-3 + 1.17e-3 * k) : 3.2 + all * (0.4e-3 + 0.25e-3 * k);
+            offer(LOZA_KERNEL_ROWS, k, false, (wide ? rounds(groups * k) * (6.5 + 1.12 * steps) : pairs ? 3.7 + 0.8 * steps : rounds(groups * k) * (3.7 + 0.55 * steps)) + merge);
+        }
+    }
+    if (wide) {
+        const int64_t tiles = (rows + loza::kTileRows - 1) / loza::kTileRows * heads;
+        const double once = rounds(tiles) * (12 + 1.45 * (keys / 32 + 2)), twice = rounds(tiles) * (12 + 2.1 * (keys / 32 + 2));
+        const bool precise = live <= 2304 && rounds(tiles) <= 2;
+        offer(LOZA_KERNEL_TILES, 1, precise, precise ? twice : once);
+        for (int64_t k = 2; k <= most && tiles * k <= 2 * kComputeUnits; ++k)
+            offer(LOZA_KERNEL_TILES, k, true, rounds(tiles * k) * (12 + 2.3 * ceil((keys / 32 + 2) / k)) + 6 + 0.45e-3 * all * k);
+    } else {
+        const int64_t tiles = (rows + 255) / 256 * heads;
+        const bool half = rows <= 128;                     // of the waves have no row
+        offer(LOZA_KERNEL_D128, 1, false, rounds(tiles) * (11 + (half ? 0.021 : 0.0275) * keys));
+        for (int64_t k = 2; k <= most && tiles * k <= 2 * kComputeUnits; ++k)
+            offer(LOZA_KERNEL_D128, k, true, rounds(tiles * k) * (9 + (half ? 0.03 : 0.036) * (keys / k + 64)) + 8 + 0.11e-3 * all * k);
+    }
+    return best;
+}
+
 // The reference maximum of the online softmax moves only when exceeded by more than 2^8 (fp32 has the headroom).
 // Over the first 8 key tiles the tile kernel keeps it exact (its wide prefill over the first only); the few-rows
 // and the width-128 kernel, which do not read exact_tiles, over their first tile or step.
@@ -375,7 +427,19 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
     set_rescale_policy(p);
     bool few_rows = loza::few_rows_bf16(B, Hkv, (extend ? q_len : S) * G);
     if (extend) {
-        if (scratch) {
+        if (tree_masks) {
+            const TreePlan plan = tree_plan(B, Hkv, G, q_len, S, d_qk, pat, scratch);
+            if (plan.n_splits > 1) {
+                if (workspace_bytes < split_bytes(B, Hq, q_len, d_v, plan.n_splits)) return LOZA_ERR_WORKSPACE;
+                if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
+                p.part_o = (float *)workspace;
+                p.part_ml = (float *)workspace + (size_t)B * Hq * q_len * plan.n_splits * d_v;
+            }
+            few_rows = plan.kernel == LOZA_KERNEL_ROWS;
+            p.n_splits = plan.n_splits;
+            p.all_precise = plan.precise;
+            p.tree_lens = tree_lens; p.tree_masks = tree_masks;
+        } else if (scratch) {
             auto held = [&](int n) { return n == 1 || (workspace && workspace_bytes >= split_bytes(B, Hq, q_len, d_v, n)); };
             ExtendPlan plan = extend_plan(B, Hkv, G, q_len, S, d_qk, pat);
             if (!held(plan.n_splits)) plan = extend_plan(B, Hkv, G, q_len, S, d_qk, pat, true);
@@ -393,7 +457,6 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
             p.block_table = paging->block_table;
             p.page_shift = page_shift; p.max_pages = paging->max_pages; p.num_pages = (int)paging->num_pages;
         }
-        p.tree_lens = tree_lens; p.tree_masks = tree_masks;
         if (few_rows) return loza::launch_rows_bf16(p, d_qk, d_v, alias, false, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
         return loza::launch_extend_bf16(p, d_qk, d_v, alias, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
     }
@@ -1122,8 +1185,23 @@ int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int3
 size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
                                             int64_t sink_blocks, int64_t local_blocks, int64_t block)
 {
-    if (n > LOZA_TREE_MAX_NODES) return 0;
-    return loza_ssa_extend_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, sink_blocks, local_blocks, block);
+    if (check_common(B, Hq, Hkv, S_max, d_qk, d_v, sink_blocks, local_blocks, 1.0f) != LOZA_OK) return 0;
+    if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || n < 1 || n > S_max || n > LOZA_TREE_MAX_NODES) return 0;
+    if (!loza::bf16_shape_supported(d_qk, d_v, true)) return 0;
+    const int splits = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), true).n_splits;
+    return splits > 1 ? split_bytes(B, Hq, n, d_v, splits) : 0;
+}
+
+int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int64_t sink_blocks, int64_t local_blocks,
+                                int64_t block, int scratch, int *n_splits)
+{
+    if (int rc = check_common(B, Hq, Hkv, S_max, d_qk, 1, sink_blocks, local_blocks, 1.0f)) return rc;
+    if (int rc = check_blocks(sink_blocks, local_blocks, block)) return rc;
+    if (n < 1 || n > S_max || n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    if (!loza::bf16_width_supported(d_qk)) return LOZA_ERR_UNSUPPORTED;
+    const TreePlan plan = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), scratch != 0);
+    if (n_splits) *n_splits = plan.n_splits;
+    return plan.kernel;
 }
 
 int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,

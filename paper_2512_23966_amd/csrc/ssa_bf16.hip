@@ -1093,7 +1093,7 @@ __global__ __launch_bounds__(DV / 4) void ssa_decode_merge_kernel(const FwdParam
 // A pattern that leaves rows beyond the first kPrecisePositions positions with fewer live keys than
 // that takes the two-term variant throughout. The smallest live set of such a row is at position
 // kPrecisePositions - 1 or at the first query of a block whose window has reached full length.
-static bool pattern_needs_precise(int64_t S, int n_sink, int window, int block)
+bool pattern_needs_precise(int64_t S, int n_sink, int window, int block)
 {
     auto live_at = [&](int64_t i) {
         const int64_t se = n_sink < i + 1 ? n_sink : i + 1;
@@ -1142,6 +1142,15 @@ __global__ __launch_bounds__(256) void ssa_split_add_kernel(const FwdParams p)
     }
 }
 
+hipError_t launch_split_add(const FwdParams &p, int d_v, hipStream_t stream)
+{
+    const int64_t threads = (int64_t)p.B * p.q_len * p.Hq * (d_v / 8);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (d_v == 512) hipLaunchKernelGGL(ssa_split_add_kernel<512>, grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(ssa_split_add_kernel<128>, grid, dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
 template <int DQK, int DV, bool ALIAS, bool OUTF32, bool EXT, bool SPLIT = false, bool TREE = false>
 static hipError_t launch_prefill_kernel(FwdParams p, hipStream_t stream)
 {
@@ -1150,7 +1159,7 @@ static hipError_t launch_prefill_kernel(FwdParams p, hipStream_t stream)
     hipError_t e = allow_lds<kern>(C::LDS_BYTES);
     if (e != hipSuccess) return e;
     p.rt_begin = 0;
-    p.all_precise = pattern_needs_precise(p.S, p.n_sink, p.window, p.block) ? 1 : 0;
+    p.all_precise = (TREE && p.all_precise) || pattern_needs_precise(p.S, p.n_sink, p.window, p.block) ? 1 : 0;
     // The speculative softmax scores a tile twice when the reference moves: the reference is exact
     // over the first tile only, afterwards lazy (with an exact reference over the first 8 tiles most
     // of them would move it).
@@ -1158,13 +1167,8 @@ static hipError_t launch_prefill_kernel(FwdParams p, hipStream_t stream)
     const int64_t blocks = (int64_t)p.row_tiles * p.Hkv * p.B * (SPLIT ? p.n_splits : 1);
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), C::LDS_BYTES, stream, p);
     e = hipGetLastError();
-    if constexpr (SPLIT) {
-        if (e != hipSuccess) return e;
-        const int64_t threads = (int64_t)p.B * p.q_len * p.Hq * (DV / 8);
-        hipLaunchKernelGGL(ssa_split_add_kernel<DV>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p);
-        e = hipGetLastError();
-    }
-    return e;
+    if (!SPLIT || e != hipSuccess) return e;
+    return launch_split_add(p, DV, stream);
 }
 
 template <int DQK, int DV, bool ALIAS>
@@ -1178,9 +1182,11 @@ static hipError_t launch_prefill_t(const FwdParams &p, hipStream_t stream)
 template <int DQK, int DV, bool ALIAS>
 static hipError_t launch_extend_t(const FwdParams &p, hipStream_t stream)
 {
-    if (p.tree_masks)
-        return p.n_splits > 1 ? launch_prefill_kernel<DQK, DV, ALIAS, false, true, true, true>(p, stream)
-                              : launch_prefill_kernel<DQK, DV, ALIAS, false, true, false, true>(p, stream);
+    if constexpr (DQK > 128) {                     // (trees of width 128 go to ssa_d128.hip)
+        if (p.tree_masks)
+            return p.n_splits > 1 ? launch_prefill_kernel<DQK, DV, ALIAS, false, true, true, true>(p, stream)
+                                  : launch_prefill_kernel<DQK, DV, ALIAS, false, true, false, true>(p, stream);
+    }
     if (p.n_splits > 1) return launch_prefill_kernel<DQK, DV, ALIAS, false, true, true>(p, stream);
     return launch_prefill_kernel<DQK, DV, ALIAS, false, true>(p, stream);
 }
@@ -1373,7 +1379,7 @@ hipError_t launch_extend_bf16(const FwdParams &p, int d_qk, int d_v, bool alias,
 {
     if (d_qk == 576 && d_v == 512 && alias) return launch_extend_t<576, 512, true>(p, stream);
     if (d_qk == 128 && d_v == 128) {
-        if (d128_tiles_pay(p)) return launch_d128_bf16(p, alias, stream);
+        if (p.tree_masks || d128_tiles_pay(p)) return launch_d128_bf16(p, alias, stream);
         return alias ? launch_extend_t<128, 128, true>(p, stream) : launch_extend_t<128, 128, false>(p, stream);
     }
     return hipErrorInvalidValue;

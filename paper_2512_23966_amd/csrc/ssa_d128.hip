@@ -60,8 +60,9 @@ struct D128Cfg {
 
 // One pass over one workgroup tile. PRECISE: two-term weights. Returns true (the same in every wave) when the
 // tile has been left unwritten for a PRECISE pass.
-// TREE: the queries are the nodes of a tree (ssa_tree.h).
-template <bool ALIAS, bool PRECISE, bool OUTF32, bool TREE>
+// TREE: the queries are the nodes of a tree (ssa_tree.h). SPLIT (trees): the workgroup takes every n_splits-th stage of keys and leaves fp32
+// partial results, which ssa_split_add_kernel adds; always PRECISE (which rows have a large result is not known before).
+template <bool ALIAS, bool PRECISE, bool OUTF32, bool TREE, bool SPLIT>
 static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *smem)
 {
     using C = D128Cfg<ALIAS>;
@@ -70,8 +71,11 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, ln = lane & 31, lh = lane >> 5;
 
     // ---- which tile of which (batch, kv head): every XCD takes one contiguous eighth (see ssa_bf16.hip) ----
-    int id = blockIdx.x;
-    {
+    int id = blockIdx.x, split = 0;
+    if constexpr (SPLIT) {
+        split = id % p.n_splits;
+        id /= p.n_splits;
+    } else {
         const int total = gridDim.x, chunk = total / 8;
         if (id < chunk * 8) id = (id % 8) * chunk + id / 8;
     }
@@ -90,11 +94,12 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     const int i_min = TREE ? (int)span.P - 1 : (int)(pos0 + row_position(r0, G));
     const int i_max = TREE ? (padding ? -1 : (int)span.L - 1) : (int)(pos0 + row_position(last_row(r0, M), G));
     const int i_low = TREE ? (int)span.P : i_min;
-    if (!PRECISE && i_low < kPrecisePositions) return true;
+    if (!PRECISE && (i_low < kPrecisePositions || (TREE && p.all_precise))) return true;
 
     // positions of this wave's rows
     const int64_t w0 = r0 + wave * 32 < R ? r0 + wave * 32 : R - 1;
-    const int wi_min = TREE ? i_min : (int)(pos0 + row_position(w0, G)), wi_max = TREE ? i_max : (int)(pos0 + row_position(last_row(w0, 32), G));
+    const int wi_min = TREE ? i_min : (int)(pos0 + row_position(w0, G));
+    const int wi_max = TREE ? (row_position(w0, G) >= span.nodes ? -1 : i_max) : (int)(pos0 + row_position(last_row(w0, 32), G));
     const int wi_low = TREE ? i_low : wi_min;
     const int w_lo_min = window_begin_of(wi_low < 0 ? 0 : wi_low, window, block);
     const int w_lo_max = window_begin_of(wi_max < 0 ? 0 : wi_max, window, block);
@@ -107,10 +112,11 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     int nB;
     if (wt0 <= nA) { nA = wt1 + 1; nB = 0; } else { nB = wt1 - wt0 + 1; }
     if (i_max < 0) { nA = 0; nB = 0; }
-    const int nt = nA + nB;
+    const int nt = SPLIT ? (nA + nB > split ? (nA + nB - split + p.n_splits - 1) / p.n_splits : 0) : nA + nB;
     int w_rot = 0;
-    if (nB > 1) { w_rot = wt0 % nB; w_rot = w_rot == 0 ? 0 : nB - w_rot; }
+    if (!SPLIT && nB > 1) { w_rot = wt0 % nB; w_rot = w_rot == 0 ? 0 : nB - w_rot; }
     auto key_tile = [&](int t) {
+        if (SPLIT) t = split + t * p.n_splits;
         if (t < nA) return t;
         int x = t - nA + w_rot;
         x = x >= nB ? x - nB : x;
@@ -325,6 +331,33 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     // ---- epilogue --------------------------------------------------------------------------------------------
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may be on its way into LDS any more
     lds_barrier();                                     // the stages are no longer read
+    if constexpr (SPLIT) {
+        const float l1 = l_run[0] + l_run[1], l = l1 + xor32(l1);
+        const bool nothing = i_row == kNothing;            // (stages that take no mask have been added to its sums)
+        const int64_t row = r0 + wave * 32 + ln;
+        if (row < R) {
+            const int64_t i = row_position(row, G);
+            const int64_t at = (((int64_t)b * Sq + i) * p.Hq + (int64_t)g * G + (row - i * G)) * p.n_splits + split;
+            if (lh == 0) {
+                p.part_ml[at * 4 + 0] = nothing ? LOZA_NEG_INF : m_ref;
+                p.part_ml[at * 4 + 1] = nothing ? 0.f : l;
+                p.part_ml[at * 4 + 2] = nothing ? 0.f : osum[0];
+            }
+            float *op = p.part_o + at * D + 4 * lh;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int qd = 0; qd < 4; ++qd) {
+                    float4 w;
+                    w.x = o[db][4 * qd + 0];
+                    w.y = o[db][4 * qd + 1];
+                    w.z = o[db][4 * qd + 2];
+                    w.w = o[db][4 * qd + 3];
+                    *(float4 *)(op + db * 32 + qd * 8) = w;
+                }
+        }
+        return false;
+    }
     bool big = false;
     float inv, lse;
     {
@@ -410,29 +443,38 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     return false;
 }
 
-template <bool ALIAS, bool OUTF32, bool TREE>
+template <bool ALIAS, bool OUTF32, bool TREE, bool SPLIT>
 __global__ __launch_bounds__(512, 2) void ssa_d128_kernel(const FwdParams p)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    if (ssa_d128_tile<ALIAS, false, OUTF32, TREE>(p, smem)) ssa_d128_tile<ALIAS, true, OUTF32, TREE>(p, smem);
+    if constexpr (SPLIT) ssa_d128_tile<ALIAS, true, OUTF32, TREE, true>(p, smem);
+    else if (ssa_d128_tile<ALIAS, false, OUTF32, TREE, false>(p, smem)) ssa_d128_tile<ALIAS, true, OUTF32, TREE, false>(p, smem);
 }
 
-template <bool ALIAS, bool OUTF32, bool TREE = false>
+template <bool ALIAS, bool OUTF32, bool TREE = false, bool SPLIT = false>
 static hipError_t launch_d128_t(FwdParams p, hipStream_t stream)
 {
     using C = D128Cfg<ALIAS>;
-    constexpr auto kern = ssa_d128_kernel<ALIAS, OUTF32, TREE>;
+    constexpr auto kern = ssa_d128_kernel<ALIAS, OUTF32, TREE, SPLIT>;
     hipError_t e = allow_lds<kern>(C::LDS_BYTES);
     if (e != hipSuccess) return e;
     const int64_t rows = (p.seqlens ? (int64_t)p.q_len : p.S) * p.G;
     p.row_tiles = (int)((rows + C::M - 1) / C::M);
-    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)p.row_tiles * p.Hkv * p.B)), dim3(64 * C::NW), C::LDS_BYTES, stream, p);
-    return hipGetLastError();
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)p.row_tiles * p.Hkv * p.B * p.n_splits)), dim3(64 * C::NW), C::LDS_BYTES, stream, p);
+    e = hipGetLastError();
+    if (!SPLIT || e != hipSuccess) return e;
+    return launch_split_add(p, C::D, stream);
 }
 
 hipError_t launch_d128_bf16(const FwdParams &p, bool alias, hipStream_t stream)
 {
-    if (p.tree_masks) return alias ? launch_d128_t<true, false, true>(p, stream) : launch_d128_t<false, false, true>(p, stream);
+    if (p.tree_masks) {
+        // (prefills and extends come here with patterns of at least 256 live keys, trees with any)
+        FwdParams t = p;
+        t.all_precise = pattern_needs_precise(p.S, p.n_sink, p.window, p.block) ? 1 : 0;
+        if (p.n_splits > 1) return alias ? launch_d128_t<true, false, true, true>(t, stream) : launch_d128_t<false, false, true, true>(t, stream);
+        return alias ? launch_d128_t<true, false, true>(t, stream) : launch_d128_t<false, false, true>(t, stream);
+    }
     if (p.out_f32 != nullptr) return alias ? launch_d128_t<true, true>(p, stream) : launch_d128_t<false, true>(p, stream);
     return alias ? launch_d128_t<true, false>(p, stream) : launch_d128_t<false, false>(p, stream);
 }

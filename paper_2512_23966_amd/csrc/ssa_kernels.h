@@ -36,12 +36,12 @@ struct FwdParams {
     int rt_begin;      // first of them
     int n_splits;      // decode and extend: workgroups that share the keys of a row (1: no partial results)
     int q_len;         // extend prefill: queries per sequence (0: plain prefill); keys valid up to seqlens[b]
+    int all_precise;   // tile kernels, prefill / extend: every tile takes the two-term pass (set by the launcher from the pattern; a tree's caller may ask for it)
+    int exact_tiles;   // tile kernel: tiles over which the reference maximum is the exact running maximum
+    float lazy_log2;   // afterwards it moves only when exceeded by this much (log2 units)
     // a tree of drafted tokens (extend, else nullptr): the nodes of each sequence, q_len at most, and what each sees (ssa_tree.h)
     const int32_t *tree_lens;
     const int64_t *tree_masks;
-    int all_precise;   // tile kernel, prefill / extend: every tile takes the two-term pass (set by the launcher from the pattern)
-    int exact_tiles;   // tile kernel: tiles over which the reference maximum is the exact running maximum
-    float lazy_log2;   // afterwards it moves only when exceeded by this much (log2 units)
 };
 
 // The tile kernels use more dynamic LDS than the default limit: raised once per kernel and device.
@@ -65,8 +65,12 @@ int decode_rows_per_tile();
 hipError_t launch_prefill_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
 hipError_t launch_extend_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
 hipError_t launch_decode_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
+// Second launch of a call whose tiles are split over their keys: adds the partial results
+hipError_t launch_split_add(const FwdParams &p, int d_v, hipStream_t stream);
 // Heads of width 128, many query rows (ssa_d128.hip): prefill (seqlens null) or extend.
 hipError_t launch_d128_bf16(const FwdParams &p, bool alias, hipStream_t stream);
+// A pattern that leaves rows with so few live keys that tiles take two-term weights throughout
+bool pattern_needs_precise(int64_t S, int n_sink, int window, int block);
 bool d128_tiles_pay(int B, int Hkv, int G, int64_t queries, int64_t S, int n_sink, int window, int block);
 // Few query rows (ssa_rows.hip): prefill (seqlens null), extend or decode (q_len = 1; n_splits key splits
 // and a merge; weights that are not rounded at all).

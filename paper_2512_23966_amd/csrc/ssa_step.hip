@@ -477,7 +477,7 @@ void verify_plan(VerifyParams &p, bool draft)
     if (slices > ((int64_t)p.V + 1023) / 1024) slices = ((int64_t)p.V + 1023) / 1024;
     p.slice_len = (int)(((p.V + slices - 1) / slices + 63) / 64 * 64);
     p.slices = (p.V + p.slice_len - 1) / p.slice_len;
-    p.rounds = draft && p.n > 2 ? 2 : 1;
+    p.rounds = !draft || p.n <= 2 ? 1 : p.n <= 16 ? 2 : 3;
     p.quads = p.V % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.target) | reinterpret_cast<uintptr_t>(p.draft)) & 15u) == 0;
 }
 

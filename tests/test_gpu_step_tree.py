@@ -123,6 +123,83 @@ def test_masks_that_are_no_trees(gpu_device, d, Hq, Hkv):
         _check(q, kc, kc, lens, counts, masks, out, lse, sink, local, block, scale, f"any masks, window {local}", [0, Hq - 1], 1)
 
 
+# the kernels of larger calls: B, Hq, Hkv, d, S_max, n, sink, local, block, page, values are the keys, (kernel, splits > 1), step of the nodes compared
+LARGE = [
+    (5, 64, 1, 576, 6144, 33, 128, 5000, 1, 0, True, (loza.KERNEL_TILES, True), 16),
+    (2, 64, 1, 576, 4096, 64, 1, 20, 128, 128, True, (loza.KERNEL_TILES, True), 31),
+    (5, 128, 2, 576, 4900, 63, 64, 4600, 1, 0, True, (loza.KERNEL_TILES, False), 31),     # weights of one term
+    (3, 192, 1, 576, 1500, 61, 1, 7, 128, 0, True, (loza.KERNEL_TILES, False), 30),       # of two throughout; 192 heads: tiles across nodes
+    (1, 64, 1, 576, 5000, 7, 128, 4500, 1, 0, True, (loza.KERNEL_ROWS, True), 2),
+    (4, 32, 8, 128, 600, 33, 16, 256, 1, 64, False, (loza.KERNEL_ROWS, False), 16),       # pairs of row groups
+    (4, 32, 8, 128, 600, 33, 16, 256, 1, 0, True, (loza.KERNEL_ROWS, False), 16),
+    (1, 12, 4, 128, 4500, 21, 16, 4300, 1, 0, True, (loza.KERNEL_ROWS, True), 10),
+    (8, 32, 8, 128, 4400, 37, 64, 4096, 1, 0, False, (loza.KERNEL_D128, True), 18),
+    (4, 48, 8, 128, 4416, 61, 1, 60, 64, 32, False, (loza.KERNEL_D128, True), 20),        # 6 heads a group
+    (8, 32, 8, 128, 4400, 40, 64, 4096, 1, 0, True, (loza.KERNEL_D128, True), 39),
+    (16, 32, 8, 128, 700, 64, 16, 512, 1, 0, True, (loza.KERNEL_D128, False), 63),
+    (20, 32, 8, 128, 320, 60, 2, 20, 1, 32, False, (loza.KERNEL_D128, False), 29),        # so few live keys that weights have two terms
+    (40, 16, 8, 128, 300, 64, 0, 200, 1, 0, False, (loza.KERNEL_D128, False), 63),        # half a tile
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,S_max,n,sink,local,block,page,alias,kernel,step", LARGE)
+def test_tree_attention_by_kernel(gpu_device, B, Hq, Hkv, d, S_max, n, sink, local, block, page, alias, kernel, step):
+    got, splits = loza.loza_ssa_extend_tree_kernel(B, Hq, Hkv, S_max, n, d, sink, local, block)
+    assert (got, splits > 1) == kernel
+    rng = np.random.default_rng(n * 1000 + S_max)
+    lens = [S_max, n - 2, S_max - 77, S_max // 2 + 5, 127 + n] + [S_max - 13 * b % 200 for b in range(5, B)]
+    counts = [n, n, n - 1, max(1, n // 2), n] + [max(1, n - b) for b in range(5, B)]
+    lens, counts = lens[:B], [min(c, x) for c, x in zip(counts[:B], lens)]
+    q, kc = _rand((B, n, Hq, d), 11, gpu_device), _rand((B, S_max, Hkv, d), 12, gpu_device)
+    vc = kc if alias else _rand((B, S_max, Hkv, d), 13, gpu_device)
+    d_v, scale = (512, 192 ** -0.5) if d == 576 else (128, 128 ** -0.5)
+    masks = _masks(rng, n, counts, "tree")
+    masks[0, n // 3] = 0                                   # a node without a mask, and one that does not see itself
+    masks[0, n // 2] &= np.uint64(0xFFFFFFFFFFFFFFFF ^ (1 << (n // 2)))
+    for b, L in enumerate(lens):
+        kc[b, L:] = float("nan")
+        vc[b, L:] = float("nan")
+    out, lse = _call(q, kc, vc, lens, counts, masks, sink, local, block, scale, d_v, page)
+    heads = sorted({0, Hq // 3, Hq - 1})
+    few = list(range(min(B, 5))) + ([B - 1] if B > 5 else [])
+    k_few = kc[few]
+    _check(q[few], k_few, k_few if alias else vc[few], [lens[b] for b in few], [counts[b] for b in few], masks[few], out[few], lse[few], sink, local, block,
+           scale, f"kernel {got} in {splits} n{n}", heads, step)
+    again, lse_again = _call(q, kc, vc, lens, counts, masks, sink, local, block, scale, d_v, page)     # the same bits
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse.view(torch.int32), lse_again.view(torch.int32))
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,S_max,n,sink,local,block,page", [
+    (2, 64, 1, 576, 4096, 40, 40, 1000, 1, 32), (1, 64, 1, 576, 4096, 3, 1, 3, 128, 64), (9, 64, 1, 576, 4096, 64, 1, 7, 128, 128),
+    (8, 32, 8, 128, 4096, 40, 40, 2000, 1, 32), (16, 32, 8, 128, 2048, 60, 1, 5, 64, 32), (2, 32, 8, 128, 4096, 9, 33, 700, 1, 64)])
+def test_pages_without_a_live_key_are_not_read(gpu_device, B, Hq, Hkv, d, S_max, n, sink, local, block, page):
+    """Pages between the sink and the first window key hold NaN and their table entries are no pages."""
+    rng = np.random.default_rng(page)
+    q, kc = _rand((B, n, Hq, d), 14, gpu_device), _rand((B, S_max, Hkv, d), 15, gpu_device)
+    vc = kc if d == 576 else _rand((B, S_max, Hkv, d), 16, gpu_device)
+    d_v, scale = (512, 192 ** -0.5) if d == 576 else (128, 128 ** -0.5)
+    lens, counts = [S_max - 31 * b for b in range(B)], [n - b % 3 for b in range(B)]
+    masks = _masks(rng, n, counts, "tree")
+    pool, table = _paginate(kc, page, 6)
+    vpool = pool if vc is kc else _paginate(vc, page, 6)[0]
+    for b in range(B):
+        P = lens[b] - counts[b]
+        first = max(0, (P // block - local + 1) * block)
+        for i in range(-(-sink * block // page), first // page):
+            pool[int(table[b, i])] = float("nan")
+            vpool[int(table[b, i])] = float("nan")
+            table[b, i] = (-1, pool.shape[0] + 7, -2 ** 31)[i % 3]
+    out, lse = torch.empty(B, n, Hq, d_v, dtype=BF, device=gpu_device), torch.empty(B, Hq, n, dtype=torch.float32, device=gpu_device)
+    i32 = dict(dtype=torch.int32, device=gpu_device)
+    loza.loza_ssa_extend_tree(q, pool, vpool, torch.tensor(lens, **i32), torch.tensor(counts, **i32), torch.from_numpy(masks.view(np.int64)).to(gpu_device), out, lse,
+                              sink, local, block, scale, block_table=table)
+    torch.cuda.synchronize()
+    few = sorted({0, B - 1})
+    k_few = kc[few]
+    _check(q[few], k_few, k_few if vc is kc else vc[few], [lens[b] for b in few], [counts[b] for b in few], masks[few], out[few], lse[few], sink, local, block, scale,
+           f"dead pages, page {page}", [0, Hq - 1], max(1, n // 3))
+
+
 def test_rows_with_large_results(gpu_device):
     """Rows whose weight sits on one key of the tree, or of the cache."""
     B, n, lens, counts = 2, 64, [1500, 1400], [64, 64]
