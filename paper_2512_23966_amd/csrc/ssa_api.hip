@@ -1366,7 +1366,7 @@ size_t loza_ssa_verify_tree_workspace_bytes(int B, int n, int V)
 {
     loza::VerifyParams p{};
     if (check_verify(p, B, n, V, true) != LOZA_OK) return 0;
-    return (size_t)B * p.rounds * p.slices * sizeof(double);
+    return (size_t)B * (p.rounds > 1 ? p.rounds : 1) * p.slices * sizeof(double);
 }
 
 int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,

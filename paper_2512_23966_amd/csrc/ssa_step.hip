@@ -468,8 +468,11 @@ hipError_t launch_step_tables(const TablesParams &p, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Slices: enough workgroups to fill the chip for a few sequences, at least 1,024 tokens each. Rounds of sums by all of them: a
-// chain, or drafts that are not random, need one; with draft probabilities further ones come from further rejected children.
+// Slices: enough workgroups to fill the chip for a few sequences, at least 1,024 tokens each. Rounds of sums by all of them, a launch each of
+// 2.5 us where there is nothing to add up: none up to 65,536 probabilities a sum, which one workgroup has added up before (32,000 tokens,
+// one chain of 5 nodes 9.1 us, with a round 10.7; drafts that are not random 8.7 and 11.0). Beyond, a chain or drafts that are not random need one sum
+// (131,072 tokens, 5 nodes 17.6 us without a round, 10.9 with one; 14.1 and 11.2); wider trees of random drafts need more, as many as
+// children are rejected (16 trees of 64 nodes: no round 47 us, one 42, two 34, three 25, four 30).
 void verify_plan(VerifyParams &p, bool draft)
 {
     int64_t slices = (1024 + p.B - 1) / p.B;
@@ -477,7 +480,7 @@ void verify_plan(VerifyParams &p, bool draft)
     if (slices > ((int64_t)p.V + 1023) / 1024) slices = ((int64_t)p.V + 1023) / 1024;
     p.slice_len = (int)(((p.V + slices - 1) / slices + 63) / 64 * 64);
     p.slices = (p.V + p.slice_len - 1) / p.slice_len;
-    p.rounds = !draft || p.n <= 2 ? 1 : p.n <= 16 ? 2 : 3;
+    p.rounds = (int64_t)p.V * (draft ? 2 : 1) <= 65536 ? 0 : !draft || p.n <= 8 ? 1 : p.n <= 24 ? 2 : 3;
     p.quads = p.V % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.target) | reinterpret_cast<uintptr_t>(p.draft)) & 15u) == 0;
 }
 
