@@ -50,7 +50,7 @@ struct VerifyParams {
     double *partial;              // [B, rounds, slices] sums of the residual over slices of the vocabulary
     int B, n, V;
     int slices, slice_len, rounds;
-    bool quads;                   // rows are multiples of 16 bytes, and so are their addresses
+    bool quads;                   // rows of target and draft are alike in their alignment to 16 bytes
 };
 // slices, slice_len and rounds of a call (host arithmetic on sizes), and the bytes of `partial`
 void verify_plan(VerifyParams &p, bool draft);

@@ -257,15 +257,20 @@ struct Residual {
     __device__ __forceinline__ double at(int x) const { return weight(x, p[x], DRAFT ? q[x] : 0.f); }
 };
 
-// This wave's share of the sum over a slice, in every lane: 4 tokens a lane at a time (rows of a multiple of 4 tokens: 16-byte loads),
-// the first ones at x0 + 4 first, the next 4 step further.
+// This wave's share of the sum over the slice [x0, x1), in every lane: thread `first` of `step` takes 4 tokens at a time, in 16-byte loads
+// from the first address of that alignment on (quads: both rows have the same), and one of the up to 3 tokens before and behind those.
 template <bool DRAFT>
 __device__ __forceinline__ double wave_residual(const Residual<DRAFT> &r, bool quads, int x0, int x1, int first, int step)
 {
     double sum = 0;
     if (quads) {
+        int head = -(int)((uintptr_t)(r.p + x0) >> 2) & 3;
+        head = head < x1 - x0 ? head : x1 - x0;
+        const int tail = (x1 - x0 - head) & 3;
+        if (first < head) sum += r.at(x0 + first);
+        if (first < tail) sum += r.at(x1 - tail + first);
 #pragma unroll 4
-        for (int x = x0 + 4 * first; x < x1; x += 4 * step) {
+        for (int x = x0 + head + 4 * first; x < x1 - tail; x += 4 * step) {
             const float4 p = *(const float4 *)(r.p + x);
             float4 q = {0.f, 0.f, 0.f, 0.f};
             if constexpr (DRAFT) q = *(const float4 *)(r.q + x);
@@ -469,10 +474,11 @@ hipError_t launch_step_tables(const TablesParams &p, hipStream_t stream)
 }
 
 // Slices: enough workgroups to fill the chip for a few sequences, at least 1,024 tokens each. Rounds of sums by all of them, a launch each of
-// 2.5 us where there is nothing to add up: none up to 65,536 probabilities a sum, which one workgroup has added up before (32,000 tokens,
-// one chain of 5 nodes 9.1 us, with a round 10.7; drafts that are not random 8.7 and 11.0). Beyond, a chain or drafts that are not random need one sum
-// (131,072 tokens, 5 nodes 17.6 us without a round, 10.9 with one; 14.1 and 11.2); wider trees of random drafts need more, as many as
-// children are rejected (16 trees of 64 nodes: no round 47 us, one 42, two 34, three 25, four 30).
+// 2.5 us where there is nothing to add up, against some 10 for a sum over 131,072 tokens by one workgroup: none for up to 65,536 probabilities a
+// sum of calls whose probabilities are still in a cache when they are small enough for one (32,000 tokens, one chain of 5 nodes: 9.1 us, with a round 10.7;
+// from memory 16.7 and 14.6). A chain or drafts that are not random need one sum (131,072 tokens from memory, 16 sequences of 5 nodes: no round 36.8 us,
+// one 20.0, two 23.2); wider trees of random drafts need as many as children are rejected (16 of 16 nodes: one round 44 us, three 33,
+// four 37; one of 64: one 31, three 23, five 30; 16 of 64: one 99, three 81, five 65, six 61, eight 73).
 void verify_plan(VerifyParams &p, bool draft)
 {
     int64_t slices = (1024 + p.B - 1) / p.B;
@@ -480,8 +486,10 @@ void verify_plan(VerifyParams &p, bool draft)
     if (slices > ((int64_t)p.V + 1023) / 1024) slices = ((int64_t)p.V + 1023) / 1024;
     p.slice_len = (int)(((p.V + slices - 1) / slices + 63) / 64 * 64);
     p.slices = (p.V + p.slice_len - 1) / p.slice_len;
-    p.rounds = (int64_t)p.V * (draft ? 2 : 1) <= 65536 ? 0 : !draft || p.n <= 8 ? 1 : p.n <= 24 ? 2 : 3;
-    p.quads = p.V % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.target) | reinterpret_cast<uintptr_t>(p.draft)) & 15u) == 0;
+    const int64_t sum = (int64_t)p.V * (draft ? 2 : 1);
+    const bool cached = sum * p.B * p.n * 4 <= 64 << 20;
+    p.rounds = sum <= 65536 && cached ? 0 : !draft || p.n <= 8 ? 1 : p.n <= 24 || p.B < 8 ? 3 : 5;
+    p.quads = !draft || ((reinterpret_cast<uintptr_t>(p.target) ^ reinterpret_cast<uintptr_t>(p.draft)) & 15u) == 0;
 }
 
 template <bool DRAFT>

@@ -200,6 +200,28 @@ def _verify(dev, target, draft, tokens, parents, lens, ua, un, ws=None):
     return [x.cpu().numpy() for x in (path, pl, nx)]
 
 
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 255, 1023, 4099, 70001])
+def test_verify_rows_of_any_alignment(gpu_device, V):
+    """Probabilities that start 0 to 3 elements behind an aligned address, target and draft alike or not."""
+    rng = np.random.default_rng(V)
+    B, n = 2, 6
+    target, dr = _probs(rng, B, n, V, 1.0)
+    parents = np.stack([R.random_parents(rng, n, "star") for _ in range(B)])
+    tokens, lens = rng.integers(0, V, size=(B, n)).astype(np.int32), np.full(B, n, np.int32)
+    ua, un = rng.random((B, n), dtype=np.float32), rng.random(B, dtype=np.float32)
+    i32 = dict(dtype=torch.int32, device=gpu_device)
+    ws = torch.empty(loza.loza_ssa_verify_tree_workspace_bytes(B, n, V), dtype=torch.uint8, device=gpu_device)
+    for a, b in ((1, 1), (3, 3), (0, 2), (2, 1)):
+        at = lambda x, k: torch.cat([torch.zeros(k), torch.from_numpy(x).flatten()]).to(gpu_device)[k:].view(B, n, V)
+        for draft in (dr, None):
+            path, pl, nx = torch.full((B, n), -77, **i32), torch.full((B,), -77, **i32), torch.full((B,), -77, **i32)
+            t, d = at(target, a), None if draft is None else at(draft, b)
+            loza.loza_ssa_verify_tree(t, d, _dev(tokens, gpu_device), _dev(parents, gpu_device), _dev(lens, gpu_device), _dev(ua, gpu_device), _dev(un, gpu_device), path, pl, nx, ws)
+            torch.cuda.synchronize()
+            for g, r in zip((path, pl, nx), R.verify_tree(target, draft, tokens, parents, lens, ua, un)):
+                assert np.array_equal(g.cpu().numpy(), r), (a, b)
+
+
 def _probs(rng, B, n, V, noise):
     x = rng.standard_normal((B, n, V)) * 2
     soft = lambda z: (np.exp(z - z.max(-1, keepdims=True)) / np.exp(z - z.max(-1, keepdims=True)).sum(-1, keepdims=True)).astype(np.float32)
@@ -208,7 +230,8 @@ def _probs(rng, B, n, V, noise):
 
 @pytest.mark.parametrize("draft", [True, False])
 @pytest.mark.parametrize("B,n,V,kind,noise", [(1, 1, 1, "tree", 1), (4, 5, 7, "star", 1), (6, 64, 50, "tree", 1.5), (3, 64, 1000, "chain", 0.2), (2, 9, 32003, "tree", 0.6),
-                                              (40, 17, 333, "star", 2), (1, 6, 131072, "tree", 1), (5, 33, 4097, "tree", 0.0)])
+                                              (40, 17, 333, "star", 2), (1, 6, 131072, "tree", 1), (5, 33, 4097, "tree", 0.0),
+                                              (2, 40, 70000, "star", 1.5), (9, 30, 66000, "star", 1)])
 def test_verify(gpu_device, B, n, V, kind, noise, draft):
     rng = np.random.default_rng(B * n + V)
     target, dr = _probs(rng, B, n, V, noise)
