@@ -467,7 +467,7 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  *   masks [B, n] int64 (NULL without parents): bit a of masks[b, r] says that node r sees node a: its ancestors and itself; 0
  *           for rows without a token
  *   free_left [1] int32: valid entries of free_pages that are left
- * page_size: a power of two >= 32; num_pages * page_size < 2^31. granted, seqlens and free_left must not be the arrays they
+ * B <= 65536; page_size: a power of two >= 32; num_pages * page_size < 2^31. granted, seqlens and free_left must not be the arrays they
  * are made from (LOZA_ERR_SHAPE). The call is repeatable: it changes none of its inputs but those entries of block_table.
  */
 int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
@@ -485,7 +485,7 @@ int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, con
  *   positions [T] int32: >= 0; a token with a negative one is padding, its row of out is left as it is
  *   freq [rot_dim / 2] float64, radians per position (loza_ssa_rope_frequencies); rot_dim even, 2 .. LOZA_ROPE_MAX_DIM
  *   interleaved != 0: pair k is columns 2 k and 2 k + 1, else k and k + rot_dim / 2 (from rot_begin)
- * bf16 (loza_ssa_rope) or fp32. Base pointers need only be aligned to their elements; 16 bytes for them, the strides, d, rot_begin and (half of, where
+ * bf16 (loza_ssa_rope) or fp32. H d <= 2^30. Base pointers need only be aligned to their elements; 16 bytes for them, the strides, d, rot_begin and (half of, where
  * pairs are not interleaved) rot_dim is several times faster. Angles in 64 bits and more (exact to 2^-24 of a turn at any
  * position), sine and cosine in fp32, one rounding of each result.
  */

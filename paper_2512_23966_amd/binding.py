@@ -732,7 +732,7 @@ def loza_ssa_step_tables(cache_lens, new_lens, parents, free_pages, free_count, 
         raise ValueError("parents and masks must both be [B, n], or both None")
     _call("loza_ssa_step_tables", _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(new_lens, i32, rows, "new_lens", dev),
           _ptr(parents, i32, both, "parents", dev), _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev),
-          _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, num_pages, page_size, most,
+          _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, int(num_pages), int(page_size), most,
           _ptr(granted, i32, rows, "granted", dev), _ptr(seqlens, i32, rows, "seqlens", dev), _ptr(positions, i32, both, "positions", dev),
           _ptr(slots, i32, both, "slots", dev), _ptr(masks, torch.int64, both, "masks", dev), _ptr(free_left, i32, (1,), "free_left", dev), _stream(stream))
 
@@ -751,7 +751,7 @@ def _rope(fn_name, dtype, x, positions, freq, out, rot_begin, interleaved, mscal
     xp, xt, xh = _heads(x, dtype, shape, "x", dev)
     op, ot, oh = _heads(out, dtype, shape, "out", dev)
     _call(fn_name, xp, _ptr(positions, torch.int32, (T,), "positions", dev), _ptr(freq, torch.float64, None, "freq", dev), op, T, H, d, xt, xh, ot, oh,
-          rot_begin, 2 * pairs, bool(interleaved), bool(inverse), mscale, _stream(stream))
+          int(rot_begin), 2 * pairs, bool(interleaved), bool(inverse), float(mscale), _stream(stream))
 
 
 def loza_ssa_rope(x, positions, freq, out, rot_begin, interleaved, mscale=1.0, inverse=False, stream=None):
@@ -786,7 +786,7 @@ def _rope_append(fn_name, dtype, q, k, v, positions, slots, freq, q_out, k_rows,
     _call(fn_name, qp, kp, vp, _ptr(positions, i32, (T,), "positions", dev), _ptr(slots, i32, (T,), "slots", dev),
           _ptr(freq, torch.float64, None, "freq", dev), op, _ptr(k_rows, dtype, None, "k_rows", dev),
           _ptr(v_rows, dtype, (*lead, Hkv, d_v), "v_rows", dev), T, Hq, Hkv, d_q, d_k, d_v, qt, qh, ot, oh, kt, kh, vt, vh, rows,
-          q_rot_begin, k_rot_begin, 2 * pairs, bool(interleaved), mscale, _stream(stream))
+          int(q_rot_begin), int(k_rot_begin), 2 * pairs, bool(interleaved), float(mscale), _stream(stream))
 
 
 def loza_ssa_rope_append(q, k, v, positions, slots, freq, q_out, k_rows, v_rows, q_rot_begin, k_rot_begin, interleaved, mscale=1.0, stream=None):
@@ -830,7 +830,7 @@ def loza_ssa_extend_tree(q, kcache, vcache, seqlens, tree_lens, masks, out, lse,
         raise ValueError("kcache must be [B, S_max, Hkv, d_qk], or pages [num_pages, page_size, Hkv, d_qk] with a block_table")
     paging = (0, 0, 0) if block_table is None else (lead, size, block_table.shape[-1])
     S_max = size if block_table is None else size * paging[2]
-    pattern = (sink_blocks, _win(local_blocks), block)
+    pattern = (int(sink_blocks), _win(local_blocks), int(block))
     kp = _ptr(kcache, bf, None, "kcache", dev)
     args = (_ptr(q, bf, None, "q", dev), kp, kp if vcache is kcache else _ptr(vcache, bf, (lead, size, Hkv, d_v), "vcache", dev),
             _ptr(block_table, i32, (B, paging[2]), "block_table", dev), _ptr(seqlens, i32, (B,), "seqlens", dev), _ptr(tree_lens, i32, (B,), "tree_lens", dev),
@@ -838,7 +838,7 @@ def loza_ssa_extend_tree(q, kcache, vcache, seqlens, tree_lens, masks, out, lse,
     if workspace is None:
         need = loza_ssa_extend_tree_workspace_bytes(B, Hq, Hkv, S_max, n, d_qk, d_v, *pattern)
         workspace = _scratch(need, stream) if need else None
-    _call("loza_ssa_extend_tree", *args, B, Hq, Hkv, S_max, *paging, n, d_qk, d_v, *pattern, scale,
+    _call("loza_ssa_extend_tree", *args, B, Hq, Hkv, S_max, *paging, n, d_qk, d_v, *pattern, float(scale),
           _ptr(workspace, torch.uint8, None, "workspace", dev), 0 if workspace is None else workspace.numel(), _stream(stream))
 
 

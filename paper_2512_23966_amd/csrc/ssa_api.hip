@@ -1212,7 +1212,7 @@ int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, con
     if (!cache_lens || !new_lens || !free_count || !granted || !seqlens || !positions || !slots || !free_left) return LOZA_ERR_NULL;
     if (!free_pages && num_free > 0) return LOZA_ERR_NULL;
     if ((parents == nullptr) != (masks == nullptr)) return LOZA_ERR_NULL;
-    if (B < 1 || n < 1 || num_free < 0 || num_free > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (B < 1 || B > 65536 || n < 1 || num_free < 0 || num_free > 2147483647LL) return LOZA_ERR_SHAPE;   // (a workgroup adds up all requests before its own)
     if (parents && n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
     int shift = 0;
     int64_t capacity = 0;
@@ -1258,12 +1258,13 @@ int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t o
 static int check_heads(const loza::RopeHeads &r, int64_t T, int rot, int es, bool out_strided)
 {
     if (!r.x || !r.out) return LOZA_ERR_NULL;
-    if (r.H < 1 || r.d < 1 || r.rot_begin < 0 || (int64_t)r.rot_begin + rot > r.d) return LOZA_ERR_SHAPE;
-    if (r.x_token < 0 || r.x_head < 0) return LOZA_ERR_SHAPE;
+    if (r.H < 1 || r.d < 1 || r.rot_begin < 0 || (int64_t)r.rot_begin + rot > r.d || (int64_t)r.H * r.d > 1 << 30) return LOZA_ERR_SHAPE;
+    const int64_t big = INT64_MAX / 4;
+    if (r.x_token < 0 || r.x_head < 0 || r.x_token > big / T || r.x_head > big / r.H) return LOZA_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(r.x) | reinterpret_cast<uintptr_t>(r.out)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
     if (!out_strided) return LOZA_OK;
-    const int64_t t = r.out_token, h = r.out_head, big = INT64_MAX / 4;
-    if (t < 0 || h < 0 || t > big / T || h > big / r.H || r.x_token > big / T || r.x_head > big / r.H) return LOZA_ERR_SHAPE;
+    const int64_t t = r.out_token, h = r.out_head;
+    if (t < 0 || h < 0 || t > big / T || h > big / r.H) return LOZA_ERR_SHAPE;
     const bool heads_inside = (r.H == 1 || h >= r.d) && (T == 1 || t >= (r.H - 1) * h + r.d);
     const bool tokens_inside = (T == 1 || t >= r.d) && (r.H == 1 || h >= (T - 1) * t + r.d);
     if (!heads_inside && !tokens_inside) return LOZA_ERR_SHAPE;
@@ -1327,7 +1328,8 @@ static int rope_append(const void *q, const void *k, const void *v, const int32_
     if (k == k_rows || cache_rows < 1 || cache_rows > 2147483647LL) return LOZA_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(slots) & 3u) return LOZA_ERR_ALIGN;
     if (v) {
-        if (d_v < 1 || v_token < 0 || v_head < 0 || v == v_rows) return LOZA_ERR_SHAPE;
+        if (d_v < 1 || (int64_t)Hkv * d_v > 1 << 30 || v_token < 0 || v_head < 0 || v_token > INT64_MAX / 4 / T || v_head > INT64_MAX / 4 / Hkv ||
+            v == v_rows) return LOZA_ERR_SHAPE;
         if ((reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(v_rows)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
     }
     return loza::launch_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;

@@ -23,7 +23,7 @@ def _tables(**k):
 def test_step_tables_refusals():
     for name in ("cache", "new", "count", "table", "granted", "seqlens", "pos", "slots", "left", "free", "parents", "masks"):
         assert _tables(**{name: None}) == ERR_NULL, name
-    for bad in (dict(B=0), dict(n=0), dict(n=65), dict(num_free=-1), dict(num_pages=0), dict(page=48), dict(page=16), dict(most=0),
+    for bad in (dict(B=0), dict(B=65537), dict(n=0), dict(n=65), dict(num_free=-1), dict(num_pages=0), dict(page=48), dict(page=16), dict(most=0),
                 dict(num_pages=1 << 26), dict(granted=2 * A), dict(seqlens=A), dict(left=5 * A), dict(most=1 << 26)):
         assert _tables(**bad) == ERR_SHAPE, bad
     for name in ("cache", "new", "parents", "free", "count", "table", "granted", "seqlens", "pos", "slots", "left"):
@@ -42,7 +42,7 @@ def test_rope_refusals():
         assert _rope(**{name: None}) == ERR_NULL, name
     for bad in (dict(T=0), dict(H=0), dict(d=0), dict(rot=0), dict(rot=63), dict(rot=66), dict(begin=-2), dict(begin=2), dict(rot=1026, d=4000), dict(m=math.nan),
                 dict(m=math.inf), dict(xt=-1), dict(xh=-64), dict(ot=64, oh=64), dict(oh=32), dict(ot=0), dict(oh=64, ot=255),
-                dict(out=A, ot=320), dict(ot=1 << 61), dict(xt=1 << 61), dict(T=1 << 31)):
+                dict(out=A, ot=320), dict(ot=1 << 61), dict(xt=1 << 61), dict(T=1 << 31), dict(H=1 << 25, oh=64, ot=1 << 31)):
         assert _rope(**bad) == ERR_SHAPE, bad
     assert _rope(x=A + 1) == ERR_ALIGN and _rope(out=4 * A + 1) == ERR_ALIGN and _rope(pos=2 * A + 2) == ERR_ALIGN and _rope(freq=3 * A + 4) == ERR_ALIGN
     assert B.lib().loza_ssa_rope_f32(A + 2, 2 * A, 3 * A, 4 * A, 5, 4, 64, 256, 64, 256, 64, 0, 64, 1, 0, 1.0, None) == ERR_ALIGN
@@ -59,7 +59,7 @@ def test_rope_append_refusals():
     for name in ("k", "v", "pos", "slots", "freq", "q_out", "k_rows", "v_rows", "q"):
         assert _append(**{name: None}) == ERR_NULL, name
     for bad in (dict(T=0), dict(Hq=0), dict(Hkv=0), dict(dk=62), dict(dq=62), dict(dv=0), dict(rows=0), dict(rows=1 << 31), dict(kt=-1), dict(vt=-1), dict(oh=10),
-                dict(k=8 * A), dict(v=9 * A), dict(kb=1), dict(qb=-1), dict(rot=7)):
+                dict(k=8 * A), dict(v=9 * A), dict(kb=1), dict(qb=-1), dict(rot=7), dict(kt=1 << 61), dict(vh=1 << 61), dict(dv=1 << 30)):
         assert _append(**bad) == ERR_SHAPE, bad
     for name in ("q", "k", "v", "q_out", "k_rows", "v_rows"):
         assert _append(**{name: A * 30 + 1}) == ERR_ALIGN, name
