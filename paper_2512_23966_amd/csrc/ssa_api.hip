@@ -1182,11 +1182,18 @@ int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int3
                         tree_lens, masks);
 }
 
+// Sizes of a tree call beyond check_common's: its nodes, and as many tiles as a launch takes (as prefill_bf16 counts them)
+static int check_tree(int B, int Hq, int Hkv, int64_t S, int n)
+{
+    if (n < 1 || n > S || n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    return ((int64_t)n * (Hq / Hkv) + loza::kTileRows - 1) / loza::kTileRows * Hkv * B > 2147483647LL ? LOZA_ERR_SHAPE : LOZA_OK;
+}
+
 size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
                                             int64_t sink_blocks, int64_t local_blocks, int64_t block)
 {
     if (check_common(B, Hq, Hkv, S_max, d_qk, d_v, sink_blocks, local_blocks, 1.0f) != LOZA_OK) return 0;
-    if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || n < 1 || n > S_max || n > LOZA_TREE_MAX_NODES) return 0;
+    if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || check_tree(B, Hq, Hkv, S_max, n) != LOZA_OK) return 0;
     if (!loza::bf16_shape_supported(d_qk, d_v, true)) return 0;
     const int splits = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), true).n_splits;
     return splits > 1 ? split_bytes(B, Hq, n, d_v, splits) : 0;
@@ -1197,7 +1204,7 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
 {
     if (int rc = check_common(B, Hq, Hkv, S_max, d_qk, 1, sink_blocks, local_blocks, 1.0f)) return rc;
     if (int rc = check_blocks(sink_blocks, local_blocks, block)) return rc;
-    if (n < 1 || n > S_max || n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    if (int rc = check_tree(B, Hq, Hkv, S_max, n)) return rc;
     if (!loza::bf16_width_supported(d_qk)) return LOZA_ERR_UNSUPPORTED;
     const TreePlan plan = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), scratch != 0);
     if (n_splits) *n_splits = plan.n_splits;
