@@ -11,6 +11,7 @@
 #include "ssa_kernels.h"
 #include "ssa_schedule.h"
 #include "ssa_step.h"
+#include "ssa_tree.h"
 
 // Scratch memory of loza_ssa_decode_static: the split kernel's partial results, in the place of a
 // caller's workspace. One copy per GPU, at an address of its own on each; the name below is only a
@@ -384,6 +385,15 @@ static size_t split_bytes(int B, int Hq, int64_t q_len, int d_v, int n)
     return (size_t)B * Hq * q_len * n * ((size_t)d_v + 4) * sizeof(float);
 }
 
+// The same of a tree: rows, or blocks of 32 rows of a key head (ssa_tree.h)
+static size_t tree_bytes(int B, int Hq, int Hkv, int64_t n, int d_v, const TreePlan &plan)
+{
+    if (plan.n_splits <= 1) return 0;
+    if (plan.kernel == LOZA_KERNEL_ROWS) return split_bytes(B, Hq, n, d_v, plan.n_splits);
+    const int64_t blocks = (int64_t)B * Hkv * loza::tree_row_blocks(n * (Hq / Hkv));
+    return (size_t)(loza::tree_part_floats(blocks, plan.n_splits, d_v) + blocks * plan.n_splits * 96) * sizeof(float);
+}
+
 static int prefill_bf16(const void *q, const void *k, const void *v, void *out, float *lse,
                         int B, int Hq, int Hkv, int64_t S, int d_qk, int d_v,
                         int64_t sink, int64_t local, int64_t block, bool blocks, float scale, void *stream,
@@ -430,10 +440,11 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
         if (tree_masks) {
             const TreePlan plan = tree_plan(B, Hkv, G, q_len, S, d_qk, pat, scratch);
             if (plan.n_splits > 1) {
-                if (workspace_bytes < split_bytes(B, Hq, q_len, d_v, plan.n_splits)) return LOZA_ERR_WORKSPACE;
+                if (workspace_bytes < tree_bytes(B, Hq, Hkv, q_len, d_v, plan)) return LOZA_ERR_WORKSPACE;
                 if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
                 p.part_o = (float *)workspace;
-                p.part_ml = (float *)workspace + (size_t)B * Hq * q_len * plan.n_splits * d_v;
+                p.part_ml = (float *)workspace + (plan.kernel == LOZA_KERNEL_ROWS ? (int64_t)B * Hq * q_len * plan.n_splits * d_v
+                                                                                  : loza::tree_part_floats((int64_t)B * Hkv * loza::tree_row_blocks(q_len * G), plan.n_splits, d_v));
             }
             few_rows = plan.kernel == LOZA_KERNEL_ROWS;
             p.n_splits = plan.n_splits;
@@ -1195,8 +1206,7 @@ size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_ma
     if (check_common(B, Hq, Hkv, S_max, d_qk, d_v, sink_blocks, local_blocks, 1.0f) != LOZA_OK) return 0;
     if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || check_tree(B, Hq, Hkv, S_max, n) != LOZA_OK) return 0;
     if (!loza::bf16_shape_supported(d_qk, d_v, true)) return 0;
-    const int splits = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), true).n_splits;
-    return splits > 1 ? split_bytes(B, Hq, n, d_v, splits) : 0;
+    return tree_bytes(B, Hq, Hkv, n, d_v, tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), true));
 }
 
 int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int64_t sink_blocks, int64_t local_blocks,

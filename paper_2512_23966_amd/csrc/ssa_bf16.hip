@@ -203,6 +203,7 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
     // Tiles among the first positions, and every tile of a pattern that leaves all rows few live keys,
     // take the two-term pass right away.
     if (!DECODE && !PRECISE && (p.all_precise || i_low < kPrecisePositions)) return true;
+    if (TREE && SPLIT && padding) return false;    // (the merge knows)
 
     bf16x8 qf[DQK / 16];
 
@@ -977,6 +978,32 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
                 }
             }
         }
+    } else if constexpr (TREE) {
+        const int64_t bg = (int64_t)b * p.Hkv + g;
+        const int last = tree_row_blocks(R) - 1;
+        if (lh == 0 && rt * RB + wr <= last) {
+            float *ml = tree_part_ml(p, bg, rt * RB + wr, split) + ln;
+            ml[0] = m_ref;
+            ml[32] = s_lpart[wr * 32 + ln];
+            ml[64] = s_lpart[M + wr * 32 + ln];
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            if (rt * RB + rb > last) continue;
+            static_assert(!TREE || C::DVW == 128, "a wave owns one column block");
+            float *op = tree_part_o(p, bg, rt * RB + rb, split, vw, DV) + lane * 4;
+#pragma unroll
+            for (int db = 0; db < C::DVB; ++db)
+#pragma unroll
+                for (int qd = 0; qd < 4; ++qd) {
+                    float4 w;
+                    w.x = o[db][rb][4 * qd + 0];
+                    w.y = o[db][rb][4 * qd + 1];
+                    w.z = o[db][rb][4 * qd + 2];
+                    w.w = o[db][rb][4 * qd + 3];
+                    *(float4 *)(op + (db * 4 + qd) * 256) = w;
+                }
+        }
     } else {
         // partial result of this key split: unnormalised O (relative to m_ref), m_ref, l, rounded l
         auto part_row = [&](int64_t row) -> int64_t {          // row of `out` (flat)
@@ -1142,12 +1169,99 @@ __global__ __launch_bounds__(256) void ssa_split_add_kernel(const FwdParams p)
     }
 }
 
-hipError_t launch_split_add(const FwdParams &p, int d_v, hipStream_t stream)
+// The same for the tiles of a tree, whose partial results lie in blocks (ssa_tree.h): a workgroup takes a block of 32 rows and 128 columns. Blocks
+// without a node were not written and give 0.
+template <int DV>
+__global__ __launch_bounds__(256) void ssa_tree_add_kernel(const FwdParams p)
 {
-    const int64_t threads = (int64_t)p.B * p.q_len * p.Hq * (d_v / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    if (d_v == 512) hipLaunchKernelGGL(ssa_split_add_kernel<512>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(ssa_split_add_kernel<128>, grid, dim3(256), 0, stream, p);
+    constexpr int CB = DV / 128, ROW = 128 + 8;    // bf16 elements of a finished row in LDS, padded
+    __shared__ float s_w[64][32], s_max[8][32], s_den[2][8][32];
+    __shared__ __attribute__((aligned(16))) uint16_t s_out[32 * ROW];
+    const int tid = threadIdx.x, cb = blockIdx.x % CB, n = p.n_splits;
+    const int64_t R = (int64_t)p.q_len * p.G, per = tree_row_blocks(R), id = blockIdx.x / CB, bg = id / per;
+    const int rb = (int)(id - bg * per), b = (int)(bg / p.Hkv), g = (int)(bg % p.Hkv);
+    const TreeSpan span = tree_span(p, b);
+    const bool padding = row_position((int64_t)rb * 32, p.G) >= span.nodes;
+    // each split's weight, maximum and sums: eight groups of 32 threads, a row a thread, every eighth split
+    const int r32 = tid & 31, grp = tid >> 5;
+    const float *ml = tree_part_ml(p, bg, rb, 0) + r32;
+    float m[8], l[8], lr[8], m_all = LOZA_NEG_INF;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int s = grp + 8 * u;
+        const bool there = !padding && s < n;
+        m[u] = there ? ml[s * 96] : LOZA_NEG_INF;
+        l[u] = there ? ml[s * 96 + 32] : 0.f;
+        lr[u] = there ? ml[s * 96 + 64] : 0.f;
+        m_all = fmaxf(m_all, m[u]);
+    }
+    s_max[grp][r32] = m_all;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 8; ++u) m_all = fmaxf(m_all, s_max[u][r32]);
+    float den = 0.f, den_r = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const float a = m[u] == LOZA_NEG_INF ? 0.f : __builtin_amdgcn_exp2f(m[u] - m_all);
+        den += a * l[u];
+        den_r += a * lr[u];
+        if (grp + 8 * u < n) s_w[grp + 8 * u][r32] = a;
+    }
+    s_den[0][grp][r32] = den;
+    s_den[1][grp][r32] = den_r;
+    __syncthreads();
+    den = den_r = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        den += s_den[0][u][r32];
+        den_r += s_den[1][u][r32];
+    }
+    const float inv = den_r > 0.f ? 1.0f / den_r : 0.f;   // (of row tid & 31, which is this lane's below) a row without a live key gives 0
+    if (tid < 32 && cb == 0 && (int64_t)rb * 32 + tid < R) {
+        const int64_t row = (int64_t)rb * 32 + tid, i = row_position(row, p.G), h = (int64_t)g * p.G + (row - i * p.G);
+        p.lse[((int64_t)b * p.Hq + h) * p.q_len + i] = (m_all + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+    }
+    float4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = {0.f, 0.f, 0.f, 0.f};
+    const int lane = tid & 63, ln = lane & 31, lh = lane >> 5;
+    if (!padding) {
+        const float *po = tree_part_o(p, bg, rb, 0, cb, DV) + tid * 4;
+#pragma unroll 4
+        for (int s = 0; s < n; ++s) {
+            const float a = s_w[s][ln];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 v = *(const float4 *)(po + (int64_t)s * CB * kBlockFloats + j * 1024);
+                x[j].x += a * v.x; x[j].y += a * v.y; x[j].z += a * v.z; x[j].w += a * v.w;
+            }
+        }
+    }
+    // instruction i = (tid + 256 j) / 64 of the block: columns 32 (i / 4) + 8 (i % 4) + 4 lh .. of row ln
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = (tid >> 6) + 4 * j;
+        u32x2 w;
+        w[0] = pack_bf16(x[j].x * inv, x[j].y * inv);
+        w[1] = pack_bf16(x[j].z * inv, x[j].w * inv);
+        *(u32x2 *)(s_out + ln * ROW + 32 * (i >> 2) + 8 * (i & 3) + 4 * lh) = w;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int at = tid + 256 * j, r = at >> 4, c = (at & 15) * 8;
+        const int64_t row = (int64_t)rb * 32 + r;
+        if (row >= R) continue;
+        const int64_t i = row_position(row, p.G), h = (int64_t)g * p.G + (row - i * p.G);
+        *(u32x4 *)(p.out + (((int64_t)b * p.q_len + i) * p.Hq + h) * DV + cb * 128 + c) = *(const u32x4 *)(s_out + r * ROW + c);
+    }
+}
+
+hipError_t launch_tree_add(const FwdParams &p, int d_v, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((int64_t)p.B * p.Hkv * tree_row_blocks((int64_t)p.q_len * p.G) * (d_v / 128)));
+    if (d_v == 512) hipLaunchKernelGGL(ssa_tree_add_kernel<512>, grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(ssa_tree_add_kernel<128>, grid, dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -1167,8 +1281,14 @@ static hipError_t launch_prefill_kernel(FwdParams p, hipStream_t stream)
     const int64_t blocks = (int64_t)p.row_tiles * p.Hkv * p.B * (SPLIT ? p.n_splits : 1);
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), C::LDS_BYTES, stream, p);
     e = hipGetLastError();
-    if (!SPLIT || e != hipSuccess) return e;
-    return launch_split_add(p, DV, stream);
+    if constexpr (SPLIT) {
+        if (e != hipSuccess) return e;
+        if constexpr (TREE) return launch_tree_add(p, DV, stream);
+        const int64_t threads = (int64_t)p.B * p.q_len * p.Hq * (DV / 8);
+        hipLaunchKernelGGL(ssa_split_add_kernel<DV>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 template <int DQK, int DV, bool ALIAS>

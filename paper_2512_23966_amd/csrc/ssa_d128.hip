@@ -61,7 +61,7 @@ struct D128Cfg {
 // One pass over one workgroup tile. PRECISE: two-term weights. Returns true (the same in every wave) when the
 // tile has been left unwritten for a PRECISE pass.
 // TREE: the queries are the nodes of a tree (ssa_tree.h). SPLIT (trees): the workgroup takes every n_splits-th stage of keys and leaves fp32
-// partial results, which ssa_split_add_kernel adds; always PRECISE (which rows have a large result is not known before).
+// partial results (blocks of ssa_tree.h), which ssa_tree_add_kernel adds; always PRECISE (which rows have a large result is not known before).
 template <bool ALIAS, bool PRECISE, bool OUTF32, bool TREE, bool SPLIT>
 static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *smem)
 {
@@ -95,6 +95,7 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     const int i_max = TREE ? (padding ? -1 : (int)span.L - 1) : (int)(pos0 + row_position(last_row(r0, M), G));
     const int i_low = TREE ? (int)span.P : i_min;
     if (!PRECISE && (i_low < kPrecisePositions || (TREE && p.all_precise))) return true;
+    if (SPLIT && padding) return false;            // (the merge knows)
 
     // positions of this wave's rows
     const int64_t w0 = r0 + wave * 32 < R ? r0 + wave * 32 : R - 1;
@@ -334,16 +335,16 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
     if constexpr (SPLIT) {
         const float l1 = l_run[0] + l_run[1], l = l1 + xor32(l1);
         const bool nothing = i_row == kNothing;            // (stages that take no mask have been added to its sums)
-        const int64_t row = r0 + wave * 32 + ln;
-        if (row < R) {
-            const int64_t i = row_position(row, G);
-            const int64_t at = (((int64_t)b * Sq + i) * p.Hq + (int64_t)g * G + (row - i * G)) * p.n_splits + split;
+        const int64_t bg = (int64_t)b * p.Hkv + g;
+        const int rb = rt * C::NW + wave;
+        if (rb < tree_row_blocks(R)) {
             if (lh == 0) {
-                p.part_ml[at * 4 + 0] = nothing ? LOZA_NEG_INF : m_ref;
-                p.part_ml[at * 4 + 1] = nothing ? 0.f : l;
-                p.part_ml[at * 4 + 2] = nothing ? 0.f : osum[0];
+                float *ml = tree_part_ml(p, bg, rb, split) + ln;
+                ml[0] = nothing ? LOZA_NEG_INF : m_ref;
+                ml[32] = nothing ? 0.f : l;
+                ml[64] = nothing ? 0.f : osum[0];
             }
-            float *op = p.part_o + at * D + 4 * lh;
+            float *op = tree_part_o(p, bg, rb, split, 0, D) + lane * 4;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -353,7 +354,7 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
                     w.y = o[db][4 * qd + 1];
                     w.z = o[db][4 * qd + 2];
                     w.w = o[db][4 * qd + 3];
-                    *(float4 *)(op + db * 32 + qd * 8) = w;
+                    *(float4 *)(op + (db * 4 + qd) * 256) = w;
                 }
         }
         return false;
@@ -463,7 +464,7 @@ static hipError_t launch_d128_t(FwdParams p, hipStream_t stream)
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)p.row_tiles * p.Hkv * p.B * p.n_splits)), dim3(64 * C::NW), C::LDS_BYTES, stream, p);
     e = hipGetLastError();
     if (!SPLIT || e != hipSuccess) return e;
-    return launch_split_add(p, C::D, stream);
+    return launch_tree_add(p, C::D, stream);
 }
 
 hipError_t launch_d128_bf16(const FwdParams &p, bool alias, hipStream_t stream)

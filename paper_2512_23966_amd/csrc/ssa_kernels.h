@@ -65,8 +65,8 @@ int decode_rows_per_tile();
 hipError_t launch_prefill_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
 hipError_t launch_extend_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
 hipError_t launch_decode_bf16(const FwdParams &p, int d_qk, int d_v, bool alias, hipStream_t stream);
-// Second launch of a call whose tiles are split over their keys: adds the partial results
-hipError_t launch_split_add(const FwdParams &p, int d_v, hipStream_t stream);
+// Second launch of a tree whose tiles are split over their keys: adds the partial results
+hipError_t launch_tree_add(const FwdParams &p, int d_v, hipStream_t stream);
 // Heads of width 128, many query rows (ssa_d128.hip): prefill (seqlens null) or extend.
 hipError_t launch_d128_bf16(const FwdParams &p, bool alias, hipStream_t stream);
 // A pattern that leaves rows with so few live keys that tiles take two-term weights throughout

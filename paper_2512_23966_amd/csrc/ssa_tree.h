@@ -59,6 +59,24 @@ __device__ __forceinline__ TreeRow tree_row(const FwdParams &p, const TreeSpan &
     return t;
 }
 
+// Partial results of tiles whose keys several workgroups share (trees): blocks of 32 rows x 128 columns as a wave's accumulators hold them, which it
+// stores 1 KB an instruction (as rows of the result, an instruction touches 32 of them: 4 sequences of 8 nodes, wide shape, 68 -> 64 us).
+// [row blocks of all (batch, key head)s][splits][column blocks][4 x 4][64 lanes][4], and of each row block and split 32 maxima, sums
+// and rounded sums.
+constexpr int kBlockFloats = 32 * 128;
+__host__ __device__ __forceinline__ int tree_row_blocks(int64_t rows) { return (int)((rows + 31) / 32); }
+__host__ __device__ __forceinline__ int64_t tree_part_floats(int64_t blocks, int n_splits, int d_v) { return blocks * n_splits * (d_v / 128) * kBlockFloats; }
+// Row block `rb` (of its (batch, key head)) of split `split`: where its columns [128 cb, 128 cb + 128) are, and its maxima and sums
+__device__ __forceinline__ float *tree_part_o(const FwdParams &p, int64_t bg, int rb, int split, int cb, int d_v)
+{
+    const int64_t block = bg * tree_row_blocks((int64_t)p.q_len * p.G) + rb;
+    return p.part_o + ((block * p.n_splits + split) * (d_v / 128) + cb) * kBlockFloats;
+}
+__device__ __forceinline__ float *tree_part_ml(const FwdParams &p, int64_t bg, int rb, int split)
+{
+    return p.part_ml + ((bg * tree_row_blocks((int64_t)p.q_len * p.G) + rb) * p.n_splits + split) * 96;
+}
+
 // Bits of nodes first .. first + 31 of a mask, those outside [0, 64) clear. (first > -2^31 + 64)
 __device__ __forceinline__ uint32_t tree_bits(uint64_t mask, int first)
 {

@@ -84,8 +84,9 @@ def test_extend_tree_refusals():
     for bad in (dict(lens=A + 2), dict(masks=A + 4), dict(seqlens=A + 2), dict(q=A + 8)):
         assert _tree(**bad) == ERR_ALIGN, bad
     need = loza.loza_ssa_extend_tree_workspace_bytes(2, 64, 1, 65536, 8, 576, 512, 128, 8192)
-    one = 2 * 64 * 8 * (512 + 4) * 4           # partial results of every row: fp32 output, maximum and sums
-    assert need >= 2 * one and need % one == 0
+    kernel, splits = loza.loza_ssa_extend_tree_kernel(2, 64, 1, 65536, 8, 576, 128, 8192)
+    rows = 2 * 64 * 8                           # fp32 output, maximum and sums of every row, in blocks of 32 rows where tiles are split
+    assert splits > 1 and need == splits * rows * ((512 + 4) * 4 if kernel == loza.KERNEL_ROWS else (512 + 3) * 4)
     assert _tree(S=65536, local=8192, ws=9 * A, ws_bytes=16) == ERR_WORKSPACE
     assert _tree(S=65536, local=8192, ws=9 * A + 8, ws_bytes=need) == ERR_ALIGN
     assert loza.loza_ssa_extend_tree_workspace_bytes(2, 64, 1, 65536, 65, 576, 512, 128, 8192) == 0
