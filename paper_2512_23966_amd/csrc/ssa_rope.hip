@@ -47,9 +47,17 @@ template <> struct Elem<float> {
 };
 template <typename E, int N> struct alignas(sizeof(E) * N) Pack { E e[N]; };
 
+// NT: past the caches (16-byte stores only)
+template <bool NT, typename P>
+__device__ __forceinline__ void store(void *at, const P &v)
+{
+    if constexpr (NT && sizeof(P) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4 *)at);
+    else *(P *)at = v;
+}
+
 // The heads of one token, by all threads of the workgroup. VEC elements a load (1: rows or columns that are not aligned to
 // 16 bytes); sc: (cos, sin) of the token's pairs.
-template <typename E, int VEC, bool INTER>
+template <typename E, int VEC, bool INTER, bool NT>
 __device__ __forceinline__ void rotate_heads(const RopeHeads &r, const E *x, E *out, int rot, const float2 *sc, bool copy_rest)
 {
     using P = Pack<E, VEC>;
@@ -62,7 +70,7 @@ __device__ __forceinline__ void rotate_heads(const RopeHeads &r, const E *x, E *
         if (u >= units) {                                            // a column outside the rotary ones
             int c = (u - units) * VEC;
             c = c < r.rot_begin ? c : c + rot;
-            *(P *)(oh + c) = *(const P *)(xh + c);
+            store<NT>(oh + c, *(const P *)(xh + c));
             continue;
         }
         if constexpr (INTER && VEC > 1) {
@@ -75,7 +83,7 @@ __device__ __forceinline__ void rotate_heads(const RopeHeads &r, const E *x, E *
                 v.e[2 * e] = Elem<E>::put(a * t.x - b * t.y);
                 v.e[2 * e + 1] = Elem<E>::put(a * t.y + b * t.x);
             }
-            *(P *)(oh + c) = v;
+            store<NT>(oh + c, v);
         } else {
             const int c0 = r.rot_begin + (INTER ? 2 * u : u * VEC), c1 = INTER ? c0 + 1 : c0 + rot / 2;
             P v = *(const P *)(xh + c0), w = *(const P *)(xh + c1);
@@ -86,13 +94,13 @@ __device__ __forceinline__ void rotate_heads(const RopeHeads &r, const E *x, E *
                 v.e[e] = Elem<E>::put(a * t.x - b * t.y);
                 w.e[e] = Elem<E>::put(a * t.y + b * t.x);
             }
-            *(P *)(oh + c0) = v;
-            *(P *)(oh + c1) = w;
+            store<NT>(oh + c0, v);
+            store<NT>(oh + c1, w);
         }
     }
 }
 
-template <typename E, int VEC, bool INTER>
+template <typename E, int VEC, bool INTER, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p, const int tokens)
 {
     extern __shared__ __attribute__((aligned(16))) float2 sc[];      // [tokens][rot / 2]
@@ -108,11 +116,11 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p, const int
         if (p.positions[tok] < 0) continue;                          // padding: nothing is written
         const float2 *s = sc + t * half;
         if (p.q.H > 0)
-            rotate_heads<E, VEC, INTER>(p.q, (const E *)p.q.x + tok * p.q.x_token, (E *)p.q.out + tok * p.q.out_token, p.rot, s, p.q.x != p.q.out);
+            rotate_heads<E, VEC, INTER, NT>(p.q, (const E *)p.q.x + tok * p.q.x_token, (E *)p.q.out + tok * p.q.out_token, p.rot, s, p.q.x != p.q.out);
         if (p.k.H == 0) continue;
         const int64_t slot = p.slots[tok];
         if (slot < 0 || slot >= p.cache_rows) continue;
-        rotate_heads<E, VEC, INTER>(p.k, (const E *)p.k.x + tok * p.k.x_token, (E *)p.k.out + slot * p.k.out_token, p.rot, s, true);
+        rotate_heads<E, VEC, INTER, false>(p.k, (const E *)p.k.x + tok * p.k.x_token, (E *)p.k.out + slot * p.k.out_token, p.rot, s, true);
         if (p.v == nullptr) continue;
         using P = Pack<E, VEC>;
         const int per = p.d_v / VEC;
@@ -123,15 +131,30 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p, const int
     }
 }
 
+template <typename E, int VEC, bool INTER>
+hipError_t launch_t(const RopeParams &p, hipStream_t stream)
+{
+    // Two tokens a workgroup (16,384 tokens of 64 heads of 64 columns, and back: one 81.3 us, two 80.8, four 86.8; 8,192 of 32 heads of
+    // 128, fp32: 82.9, 87.4, 90.3; into rows of 576: 110, 103, 101), one where there are few. Results that no cache holds, 32 MB and more, are stored
+    // past the caches (the same three 81 us in the place of 103, 87 of 130, 103 of 115).
+    const int tokens = p.T <= 2048 ? 1 : 2;
+    const dim3 grid((unsigned)((p.T + tokens - 1) / tokens));
+    const size_t lds = (size_t)tokens * (p.rot / 2) * sizeof(float2);
+    const bool past = VEC > 1 && p.k.H == 0 && p.q.x != p.q.out && p.T * p.q.H * p.q.d * (int64_t)sizeof(E) >= 32 << 20;
+    if constexpr (VEC > 1) {
+        if (past) {
+            hipLaunchKernelGGL((rope_kernel<E, VEC, INTER, true>), grid, dim3(256), lds, stream, p, tokens);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((rope_kernel<E, VEC, INTER, false>), grid, dim3(256), lds, stream, p, tokens);
+    return hipGetLastError();
+}
+
 template <typename E, int VEC>
 hipError_t launch_v(const RopeParams &p, hipStream_t stream)
 {
-    const int tokens = p.T <= 2048 ? 1 : 4;
-    const dim3 grid((unsigned)((p.T + tokens - 1) / tokens));
-    const size_t lds = (size_t)tokens * (p.rot / 2) * sizeof(float2);
-    if (p.interleaved) hipLaunchKernelGGL((rope_kernel<E, VEC, true>), grid, dim3(256), lds, stream, p, tokens);
-    else hipLaunchKernelGGL((rope_kernel<E, VEC, false>), grid, dim3(256), lds, stream, p, tokens);
-    return hipGetLastError();
+    return p.interleaved ? launch_t<E, VEC, true>(p, stream) : launch_t<E, VEC, false>(p, stream);
 }
 
 }  // namespace
