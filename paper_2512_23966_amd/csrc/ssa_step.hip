@@ -325,9 +325,9 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
     __shared__ int s_first;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const double *part = v.partial + (int64_t)b * v.rounds * v.slices;
+    const double u_next = v.u_next[b];             // (asked for before there is anything to wait for)
     Walk w;
     walk_start(w, v, b);
-    int next = -1;
     if (w.nodes > 0) {
         auto sum_here = [&]() {
             __syncthreads();
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
         }
         if (w.s > 0) {
             // the slice in which the running sum passes the threshold, then the token (every thread takes a run of tokens)
-            double thr = (double)v.u_next[b] * w.s;
+            double thr = u_next * w.s;
             double four[4], upto = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -402,7 +402,8 @@ __global__ __launch_bounds__(1024) void verify_tree_kernel(const VerifyParams v)
             if (tid == s_first) {
                 double run = base + (incl - mine);
                 int pick = -1;
-                for (int x = a; x < e; ++x) {
+                if (per == 1 && mine > 0) pick = a;
+                for (int x = pick < 0 ? a : e; x < e; ++x) {
                     const double wx = res.at(x);
                     if (!(wx > 0)) continue;
                     pick = x;
