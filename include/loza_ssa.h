@@ -532,12 +532,13 @@ int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t o
  *   q [B, n, Hq, d_qk] bf16, out [B, n, Hq, d_v] bf16, lse [B, Hq, n] fp32; 1 <= n <= LOZA_TREE_MAX_NODES, n <= S_max
  *   seqlens [B] int32: valid cache rows, the nodes' rows included, which are the last tree_lens[b] of them (a length beyond the cache is cut to it)
  *   tree_lens [B] int32: nodes of each tree, cut to [0, n] and to seqlens. Rows r >= tree_lens[b]
- *           give out = 0, lse = -inf. Cache rows at or beyond seqlens[b] are never read.
+ *           give out = 0, lse = -inf, whatever their queries hold (loza_ssa_rope_append does not write them). Cache rows at or beyond
+ *           seqlens[b] are never read.
  *   masks [B, n] int64: the nodes that node r sees (loza_ssa_step_tables makes them; its own bit has to be set if it is
  *           to see itself; bits at or beyond tree_lens[b] are ignored). With P = seqlens[b] - tree_lens[b]: node r sits at position
  *           i = P + popcount(mask) - 1 and sees cache row j < P if j is live for position i, and the node of
  *           the k-th set bit (from 0) if position P + k is. A chain's masks (bits 0 .. r) give what loza_ssa_extend
- *           gives. A mask of 0: the row sees nothing, out = 0, lse = -inf.
+ *           gives. A mask of 0: the row sees nothing, out = 0, lse = -inf, whatever its query holds.
  *   pattern, supported shapes, numerics: as loza_ssa_extend_blocks (block = 1: token-granular)
  *   workspace: as loza_ssa_extend_with_workspace, loza_ssa_extend_tree_workspace_bytes of it; NULL: no workgroups share keys
  */

@@ -745,6 +745,10 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
             const uint16_t *qp = p.q + qrow * DQK + lh * 8;
 #pragma unroll
             for (int kk = 0; kk < DQK / 16; ++kk) qf[kk] = *(const bf16x8 *)(qp + kk * 16);
+            if (TREE && !node.seen) {              // (nobody need have written it)
+#pragma unroll
+                for (int kk = 0; kk < DQK / 16; ++kk) qf[kk] = bf16x8{};
+            }
         }
         // tile 0 has landed when at most the copies of the later ones are outstanding
         if (nt < AHEAD) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -888,6 +892,7 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
             if (r0 + rb * 32 >= R) continue;                   // (chunks of a few rows a head are mostly padding)
             const float rsum = s_lpart[M + rb * 32 + ln];
             const float inv = rsum > 0.f ? 1.0f / rsum : 0.f;  // a row without a live key gives 0
+            const bool nothing = TREE && rsum == 0.f;          // (a tree's also where the values it was not to see are not finite)
             char *op = smem + (rb * 32 + ln) * C::OUTROW + (vw * C::DVW + 4 * lh) * 2;
             float mx = 0.f;
 #pragma unroll
@@ -896,7 +901,7 @@ static __device__ __forceinline__ bool ssa_fwd_tile(const FwdParams &p, char *sm
                 for (int qd = 0; qd < 4; ++qd) {
                     float x[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = o[db][rb][4 * qd + e] * inv;
+                    for (int e = 0; e < 4; ++e) x[e] = nothing ? 0.f : o[db][rb][4 * qd + e] * inv;
                     if (!PRECISE) {
                         mx = fmaxf(fmaxf(mx, __builtin_fabsf(x[0])), __builtin_fabsf(x[1]));
                         mx = fmaxf(fmaxf(mx, __builtin_fabsf(x[2])), __builtin_fabsf(x[3]));
@@ -1217,6 +1222,7 @@ __global__ __launch_bounds__(256) void ssa_tree_add_kernel(const FwdParams p)
         den_r += s_den[1][u][r32];
     }
     const float inv = den_r > 0.f ? 1.0f / den_r : 0.f;   // (of row tid & 31, which is this lane's below) a row without a live key gives 0
+    const bool nothing = den_r == 0.f;                    // (whatever its parts hold)
     if (tid < 32 && cb == 0 && (int64_t)rb * 32 + tid < R) {
         const int64_t row = (int64_t)rb * 32 + tid, i = row_position(row, p.G), h = (int64_t)g * p.G + (row - i * p.G);
         p.lse[((int64_t)b * p.Hq + h) * p.q_len + i] = (m_all + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
@@ -1242,8 +1248,8 @@ __global__ __launch_bounds__(256) void ssa_tree_add_kernel(const FwdParams p)
     for (int j = 0; j < 4; ++j) {
         const int i = (tid >> 6) + 4 * j;
         u32x2 w;
-        w[0] = pack_bf16(x[j].x * inv, x[j].y * inv);
-        w[1] = pack_bf16(x[j].z * inv, x[j].w * inv);
+        w[0] = nothing ? 0u : pack_bf16(x[j].x * inv, x[j].y * inv);
+        w[1] = nothing ? 0u : pack_bf16(x[j].z * inv, x[j].w * inv);
         *(u32x2 *)(s_out + ln * ROW + 32 * (i >> 2) + 8 * (i & 3) + 4 * lh) = w;
     }
     __syncthreads();

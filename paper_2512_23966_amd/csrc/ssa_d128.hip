@@ -193,6 +193,10 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
         const uint16_t *qp = p.q + (((int64_t)b * Sq + qi) * p.Hq + (int64_t)g * G + (rc - qi * G)) * D + lh * 8;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) qf[kk] = *(const bf16x8 *)(qp + kk * 16);
+        if (TREE && !node.seen) {                  // (nobody need have written it)
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) qf[kk] = bf16x8{};
+        }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // (with a wait the compiler sees; the first stage has landed, too)
 #pragma unroll
@@ -365,10 +369,8 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
         const float l1 = l_run[0] + l_run[1], l = l1 + xor32(l1);
         lse = (m_ref + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
         inv = osum[0] > 0.f ? 1.0f / osum[0] : 0.f;   // a row without a live key gives 0
-        if (TREE && i_row == kNothing) {               // (stages that take no mask have been added to its sums)
-            inv = 0.f;
-            lse = LOZA_NEG_INF;
-        }
+        const bool nothing = TREE && i_row == kNothing;    // (stages that take no mask have been added to its sums)
+        if (nothing) lse = LOZA_NEG_INF;
         const int row = wave * 32 + ln;
         float mx = 0.f;
         char *op = smem + row * C::OUTROW + lh * 8;
@@ -379,7 +381,7 @@ static __device__ __forceinline__ bool ssa_d128_tile(const FwdParams &p, char *s
                 float x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    x[e] = o[db][4 * qd + e] * inv;
+                    x[e] = nothing ? 0.f : o[db][4 * qd + e] * inv;
                     if (!PRECISE) mx = fmaxf(mx, __builtin_fabsf(x[e]));
                 }
                 if constexpr (!OUTF32) {

@@ -238,6 +238,12 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
     // (waited for here, with a wait the compiler sees: left to its own bookkeeping it would wait for the
     // queries inside the loop, with counts that also drain the tile copies it does not know about)
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    if constexpr (TREE) {                          // (the query of a row that sees nothing need not have been written)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) qf[mb][kk] = i_row[mb] == kNothing ? bf16x8{} : qf[mb][kk];
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -431,6 +437,7 @@ __device__ __forceinline__ void ssa_rows_pass(const FwdParams &p, char *smem, co
             lo += a * *(const f32x4 *)op;
             hi += a * *(const f32x4 *)(op + HALF * 4);
         }
+        if (TREE && l_all == 0.f) lo = hi = f32x4{0.f, 0.f, 0.f, 0.f};   // (also where the values it was not to see are not finite)
         const int64_t qi = row_position(row, G);
         const int64_t h = (int64_t)g * G + (row - qi * G);
         const int64_t o_row = ((int64_t)b * Sq + qi) * p.Hq + h;

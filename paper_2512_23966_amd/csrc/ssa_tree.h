@@ -37,7 +37,8 @@ struct TreeRow {
     bool seen;           // false: padding, or a node without a mask: it sees nothing
 };
 // In the place of the last key before the tree for a row that sees nothing. Its scores are masked where tiles are; where a tile takes no mask they
-// are not, and its sums are dropped at the end.
+// are not, and its sums and its results are dropped at the end, by a select: 0 times what a value that is not finite left would be a NaN. Its query,
+// which nobody need have written, is taken as 0: a NaN there had every tile's softmax done twice, an infinity moved the reference of the rows beside it.
 constexpr int kNothing = -2;
 
 __device__ __forceinline__ TreeRow tree_row(const FwdParams &p, const TreeSpan &s, int b, int r)
