@@ -436,13 +436,20 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  * The step around the attention: what an engine that drafts tokens calls between one decode step and the next, all of
  * it on the GPU (no lengths on the host), so that a step can be captured. The paper stretches its contexts with YaRN and
  * measures its kernels inside such an engine (Training and Efficiency sections); it describes none of this, the definitions
- * are the usual ones. A step: loza_ssa_step_tables, then in every layer loza_ssa_rope_append and loza_ssa_extend_tree
+ * are the usual ones. A step: loza_ssa_step_tables_held, then in every layer loza_ssa_rope_append and loza_ssa_extend_tree
  * (or loza_ssa_decode_paged, loza_ssa_extend_paged), then loza_ssa_verify_tree, and loza_ssa_keep_accepted for all layers.
  *
  * Trees. The tokens of a step are the nodes of a tree per sequence, at most LOZA_TREE_MAX_NODES of them, parents before their
  * children. parents[b, r] is the parent of node r, an index below r; anything else: a node without a parent. Node 0 is the
  * token that the last step ended with (its row is not in the cache yet), the others are drafts. A chain of drafts is
  * the tree parents[r] = r - 1.
+ *
+ * Pages. A page belongs to the request whose row of block_table names it until the engine puts it back on the free list, also where it holds nothing but rows
+ * that were not kept. Chunks keep all their rows; a step of drafts keeps a part of them, and leaves a request with more pages than its cache_len
+ * needs: loza_ssa_step_tables_held is told how many, and deals out new ones behind those (with loza_ssa_step_tables the engine has to put
+ * the pages [ceil((cache_len + path_len) / page_size), ceil(seqlen / page_size)) of each row back itself, or they are lost). Between two steps:
+ * cache_lens += path_lens, free_count = free_left, held = held_after. A request that ends has the first `held` entries of its row appended to
+ * free_pages at free_count, and cache_len = held = 0.
  */
 #define LOZA_TREE_MAX_NODES 64
 #define LOZA_ROPE_MAX_DIM 1024
@@ -469,11 +476,21 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  *   free_left [1] int32: valid entries of free_pages that are left
  * B <= 65536; page_size: a power of two >= 32; num_pages * page_size < 2^31. granted, seqlens and free_left must not be the arrays they
  * are made from (LOZA_ERR_SHAPE). The call is repeatable: it changes none of its inputs but those entries of block_table.
+ *
+ * loza_ssa_step_tables_held:
+ *   held [B] int32: entries of each row of block_table that are the request's pages; fewer than ceil(cache_len / page_size): taken as that many; negative
+ *           or beyond max_pages_per_seq: the request gets nothing
+ *   held_after [B] int32: the same after the call: those (as taken), and the new ones if it is served; as given where the request's numbers are not
+ *           possible. Not the array `held`.
  */
 int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
                          const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
                          int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
                          int32_t *slots, int64_t *masks, int32_t *free_left, void *stream);
+int loza_ssa_step_tables_held(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                              const int32_t *free_count, const int32_t *held, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                              int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                              int32_t *slots, int64_t *masks, int32_t *free_left, int32_t *held_after, void *stream);
 
 /*
  * Rotary positions, and their gradient. Pair k of the columns [rot_begin, rot_begin + rot_dim) of a head at position i,

@@ -39,7 +39,7 @@ EXPORTS = (
     "loza_ssa_calibration_alpha_grad", "loza_ssa_calibration_alpha_grad_workspace_bytes",
     "loza_ssa_decode_static",
     "loza_ssa_forward_kernel", "loza_ssa_decode_kernel", "loza_ssa_backward_split",
-    "loza_ssa_step_tables", "loza_ssa_rope", "loza_ssa_rope_f32", "loza_ssa_rope_append", "loza_ssa_rope_append_f32",
+    "loza_ssa_step_tables", "loza_ssa_step_tables_held", "loza_ssa_rope", "loza_ssa_rope_f32", "loza_ssa_rope_append", "loza_ssa_rope_append_f32",
     "loza_ssa_rope_frequencies", "loza_ssa_extend_tree", "loza_ssa_extend_tree_workspace_bytes",
     "loza_ssa_extend_tree_kernel",
     "loza_ssa_verify_tree", "loza_ssa_verify_tree_workspace_bytes", "loza_ssa_keep_accepted",
@@ -138,6 +138,8 @@ def lib() -> ctypes.CDLL:
         L.loza_ssa_backward_split.argtypes = [ci, ci, ci, i64, ci, ci, i64, i64, i64, ci, ctypes.POINTER(ci), ctypes.POINTER(i64)]
         L.loza_ssa_step_tables.restype = ci
         L.loza_ssa_step_tables.argtypes = [vp] * 6 + [ci, ci, i64, i64, ci, ci] + [vp] * 7
+        L.loza_ssa_step_tables_held.restype = ci
+        L.loza_ssa_step_tables_held.argtypes = [vp] * 7 + [ci, ci, i64, i64, ci, ci] + [vp] * 8
         for name in ("loza_ssa_rope", "loza_ssa_rope_f32"):
             getattr(L, name).restype = ci
             getattr(L, name).argtypes = [vp] * 4 + [i64, ci, ci] + [i64] * 4 + [ci] * 4 + [f32, vp]
@@ -721,20 +723,31 @@ def _call(fn_name, *args) -> None:
 
 
 def loza_ssa_step_tables(cache_lens, new_lens, parents, free_pages, free_count, block_table, num_pages, page_size,
-                         granted, seqlens, positions, slots, masks, free_left, stream=None):
+                         granted, seqlens, positions, slots, masks, free_left, stream=None, held=None, held_after=None):
     """Block table entries, slots, positions and (``parents`` given: the tokens are trees) ancestor masks of a step. cache_lens, new_lens,
     granted, seqlens [B], parents (or None), positions, slots [B,n], block_table [B,max_pages], free_pages [F], free_count and
-    free_left [1], all int32 on the GPU; masks [B,n] int64 (None without parents). ``block_table`` is extended in place."""
+    free_left [1], all int32 on the GPU; masks [B,n] int64 (None without parents). ``block_table`` is extended in place. held, held_after [B]
+    int32 (both or neither): pages that each request has before and after the call (``loza_ssa_step_tables_held``); a step whose rows are not
+    all kept needs them, or its requests' spare pages are dealt out anew and lost."""
     dev, i32 = _launch_device(positions), torch.int32
     B, n = positions.shape
     rows, both, (num_free,), most = (B,), (B, n), free_pages.shape, block_table.shape[-1]
     if (parents is None) != (masks is None):
         raise ValueError("parents and masks must both be [B, n], or both None")
-    _call("loza_ssa_step_tables", _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(new_lens, i32, rows, "new_lens", dev),
+    if (held is None) != (held_after is None):
+        raise ValueError("held and held_after must both be [B], or both None")
+    if held is None:
+        return _call("loza_ssa_step_tables", _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(new_lens, i32, rows, "new_lens", dev),
+                     _ptr(parents, i32, both, "parents", dev), _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev),
+                     _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, int(num_pages), int(page_size), most,
+                     _ptr(granted, i32, rows, "granted", dev), _ptr(seqlens, i32, rows, "seqlens", dev), _ptr(positions, i32, both, "positions", dev),
+                     _ptr(slots, i32, both, "slots", dev), _ptr(masks, torch.int64, both, "masks", dev), _ptr(free_left, i32, (1,), "free_left", dev), _stream(stream))
+    _call("loza_ssa_step_tables_held", _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(new_lens, i32, rows, "new_lens", dev),
           _ptr(parents, i32, both, "parents", dev), _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev),
-          _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, int(num_pages), int(page_size), most,
+          _ptr(held, i32, rows, "held", dev), _ptr(block_table, i32, (B, most), "block_table", dev), B, n, num_free, int(num_pages), int(page_size), most,
           _ptr(granted, i32, rows, "granted", dev), _ptr(seqlens, i32, rows, "seqlens", dev), _ptr(positions, i32, both, "positions", dev),
-          _ptr(slots, i32, both, "slots", dev), _ptr(masks, torch.int64, both, "masks", dev), _ptr(free_left, i32, (1,), "free_left", dev), _stream(stream))
+          _ptr(slots, i32, both, "slots", dev), _ptr(masks, torch.int64, both, "masks", dev), _ptr(free_left, i32, (1,), "free_left", dev),
+          _ptr(held_after, i32, rows, "held_after", dev), _stream(stream))
 
 
 def loza_ssa_rope_frequencies(rot_dim, base, factor=1.0, original_context=0, slow_turns=1.0, fast_turns=32.0):

@@ -1221,10 +1221,10 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
     return plan.kernel;
 }
 
-int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
-                         const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
-                         int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
-                         int32_t *slots, int64_t *masks, int32_t *free_left, void *stream)
+static int step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                       const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                       int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                       int32_t *slots, int64_t *masks, int32_t *free_left, const int32_t *held, int32_t *held_after, void *stream)
 {
     if (!cache_lens || !new_lens || !free_count || !granted || !seqlens || !positions || !slots || !free_left) return LOZA_ERR_NULL;
     if (!free_pages && num_free > 0) return LOZA_ERR_NULL;
@@ -1237,17 +1237,37 @@ int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, con
     if (num_pages * page_size > 2147483647LL) return LOZA_ERR_SHAPE;   // slots are 32-bit row numbers
     if ((int64_t)n > 65535LL * 1024) return LOZA_ERR_SHAPE;
     // a workgroup reads what another's results would be written over
-    if (granted == new_lens || seqlens == cache_lens || free_left == free_count) return LOZA_ERR_SHAPE;
+    if (granted == new_lens || seqlens == cache_lens || free_left == free_count || (held && held_after == held)) return LOZA_ERR_SHAPE;
     for (const void *ptr : {(const void *)cache_lens, (const void *)new_lens, (const void *)parents, (const void *)free_pages, (const void *)free_count,
-                            (const void *)granted, (const void *)seqlens, (const void *)positions, (const void *)slots, (const void *)free_left})
+                            (const void *)granted, (const void *)seqlens, (const void *)positions, (const void *)slots, (const void *)free_left,
+                            (const void *)held, (const void *)held_after})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if (reinterpret_cast<uintptr_t>(masks) & 7u) return LOZA_ERR_ALIGN;
     loza::TablesParams p{};
     p.cache_lens = cache_lens; p.new_lens = new_lens; p.parents = parents; p.free_pages = free_pages; p.free_count = free_count;
     p.block_table = block_table; p.granted = granted; p.seqlens = seqlens; p.positions = positions; p.slots = slots;
-    p.masks = masks; p.free_left = free_left;
+    p.masks = masks; p.free_left = free_left; p.held = held; p.held_after = held_after;
     p.B = B; p.n = n; p.page_shift = shift; p.max_pages = max_pages_per_seq; p.num_free = num_free; p.num_pages = num_pages;
     return loza::launch_step_tables(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                         const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                         int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                         int32_t *slots, int64_t *masks, int32_t *free_left, void *stream)
+{
+    return step_tables(cache_lens, new_lens, parents, free_pages, free_count, block_table, B, n, num_free, num_pages, page_size, max_pages_per_seq,
+                       granted, seqlens, positions, slots, masks, free_left, nullptr, nullptr, stream);
+}
+
+int loza_ssa_step_tables_held(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
+                              const int32_t *free_count, const int32_t *held, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
+                              int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
+                              int32_t *slots, int64_t *masks, int32_t *free_left, int32_t *held_after, void *stream)
+{
+    if (!held || !held_after) return LOZA_ERR_NULL;
+    return step_tables(cache_lens, new_lens, parents, free_pages, free_count, block_table, B, n, num_free, num_pages, page_size, max_pages_per_seq,
+                       granted, seqlens, positions, slots, masks, free_left, held, held_after, stream);
 }
 
 int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t original_context, double slow_turns,

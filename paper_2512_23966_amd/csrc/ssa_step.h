@@ -14,6 +14,8 @@ struct TablesParams {
     const int32_t *cache_lens, *new_lens, *parents, *free_pages, *free_count;
     int32_t *block_table, *granted, *seqlens, *positions, *slots, *free_left;
     int64_t *masks;
+    const int32_t *held;          // pages each request has (null: what its rows need), and what it has after the call
+    int32_t *held_after;
     int B, n, page_shift, max_pages;
     int64_t num_free, num_pages;
 };

@@ -33,7 +33,8 @@ __device__ __forceinline__ T wave_scan(T x)
 
 // ---- tables ------------------------------------------------------------------------------------------
 
-// What request b asks for: pages it holds already, and new ones (0 where its lengths are not possible).
+// What request b asks for: pages it holds already (rows that a step added and that were not kept leave it more than its cache needs),
+// and new ones (0 where its numbers are not possible).
 struct Request {
     int64_t cache, add, have, need;
     bool fits;
@@ -44,9 +45,11 @@ __device__ __forceinline__ Request request_of(const TablesParams &p, int b)
     r.cache = p.cache_lens[b];
     r.add = p.new_lens[b];
     const int64_t size = (int64_t)1 << p.page_shift;
-    r.fits = r.cache >= 0 && r.add >= 0 && r.add <= p.n && r.cache + r.add <= (int64_t)p.max_pages * size;
-    r.have = r.fits ? (r.cache + size - 1) >> p.page_shift : 0;
-    r.need = r.fits ? ((r.cache + r.add + size - 1) >> p.page_shift) - r.have : 0;
+    const int64_t held = p.held ? p.held[b] : 0;
+    r.fits = r.cache >= 0 && r.add >= 0 && r.add <= p.n && r.cache + r.add <= (int64_t)p.max_pages * size && held >= 0 && held <= p.max_pages;
+    const int64_t now = (r.cache + size - 1) >> p.page_shift, then = (r.cache + r.add + size - 1) >> p.page_shift;
+    r.have = r.fits ? (now > held ? now : held) : 0;
+    r.need = r.fits && then > r.have ? then - r.have : 0;
     return r;
 }
 
@@ -84,6 +87,7 @@ __global__ __launch_bounds__(256) void step_tables_kernel(const TablesParams p)
         if (tid == 0) {
             p.granted[b] = granted;
             p.seqlens[b] = (int32_t)(me.cache + granted);
+            if (p.held) p.held_after[b] = me.fits ? (int32_t)(me.have + (ok ? me.need : 0)) : p.held[b];
         }
     }
     const int64_t at = (int64_t)b * p.n;
