@@ -474,14 +474,14 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  *   masks [B, n] int64 (NULL without parents): bit a of masks[b, r] says that node r sees node a: its ancestors and itself; 0
  *           for rows without a token
  *   free_left [1] int32: valid entries of free_pages that are left
- * B <= 65536; page_size: a power of two >= 32; num_pages * page_size < 2^31. granted, seqlens and free_left must not be the arrays they
- * are made from (LOZA_ERR_SHAPE). The call is repeatable: it changes none of its inputs but those entries of block_table.
+ * B <= 65536; page_size: a power of two >= 32; num_pages * page_size < 2^31. No array that is written (block_table among them) may
+ * overlap another array of the call (LOZA_ERR_SHAPE). The call is repeatable: it changes none of its inputs but those entries of block_table.
  *
  * loza_ssa_step_tables_held:
  *   held [B] int32: entries of each row of block_table that are the request's pages; fewer than ceil(cache_len / page_size): taken as that many; negative
  *           or beyond max_pages_per_seq: the request gets nothing
  *   held_after [B] int32: the same after the call: those (as taken), and the new ones if it is served; as given where the request's numbers are not
- *           possible. Not the array `held`.
+ *           possible.
  */
 int loza_ssa_step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
                          const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,

@@ -1236,13 +1236,22 @@ static int step_tables(const int32_t *cache_lens, const int32_t *new_lens, const
     if (int rc = check_paging(Paging{block_table, num_pages, page_size, max_pages_per_seq}, &shift, &capacity)) return rc;
     if (num_pages * page_size > 2147483647LL) return LOZA_ERR_SHAPE;   // slots are 32-bit row numbers
     if ((int64_t)n > 65535LL * 1024) return LOZA_ERR_SHAPE;
-    // a workgroup reads what another's results would be written over
-    if (granted == new_lens || seqlens == cache_lens || free_left == free_count || (held && held_after == held)) return LOZA_ERR_SHAPE;
     for (const void *ptr : {(const void *)cache_lens, (const void *)new_lens, (const void *)parents, (const void *)free_pages, (const void *)free_count,
                             (const void *)granted, (const void *)seqlens, (const void *)positions, (const void *)slots, (const void *)free_left,
                             (const void *)held, (const void *)held_after})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if (reinterpret_cast<uintptr_t>(masks) & 7u) return LOZA_ERR_ALIGN;
+    // a workgroup reads what another's results would be written over: no result may lie on anything else
+    const int64_t b4 = 4LL * B, bn4 = b4 * n;
+    const struct { const void *ptr; int64_t bytes; } arrays[] = {
+        {granted, b4}, {seqlens, b4}, {positions, bn4}, {slots, bn4}, {masks, 2 * bn4}, {free_left, 4}, {held_after, b4}, {block_table, b4 * max_pages_per_seq},
+        {cache_lens, b4}, {new_lens, b4}, {parents, bn4}, {free_pages, 4 * num_free}, {free_count, 4}, {held, b4}};
+    constexpr int n_results = 8, n_arrays = 14;
+    for (int i = 0; i < n_results; ++i)
+        for (int j = i + 1; j < n_arrays; ++j) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(arrays[i].ptr), y = reinterpret_cast<uintptr_t>(arrays[j].ptr);
+            if (x && y && (x <= y ? y - x < (uintptr_t)arrays[i].bytes : x - y < (uintptr_t)arrays[j].bytes)) return LOZA_ERR_SHAPE;
+        }
     loza::TablesParams p{};
     p.cache_lens = cache_lens; p.new_lens = new_lens; p.parents = parents; p.free_pages = free_pages; p.free_count = free_count;
     p.block_table = block_table; p.granted = granted; p.seqlens = seqlens; p.positions = positions; p.slots = slots;

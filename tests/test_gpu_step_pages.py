@@ -58,3 +58,30 @@ def test_no_page_is_lost(gpu_device, B, n, page, most, pages, tree):
     for _ in range(300):
         pool.step(n, tree)
     assert pool.ended > 3
+
+
+def test_arrays_side_by_side(gpu_device):
+    """All arrays of a call one behind the other in one buffer: nothing overlaps, and nothing is written beside its place."""
+    B, n, page, most, num_pages = 5, 6, 32, 7, 40
+    rng = np.random.default_rng(4)
+    cache, new = rng.integers(0, 150, size=B).astype(np.int32), rng.integers(0, n + 1, size=B).astype(np.int32)
+    held, free = (-(-cache // page) + 1).astype(np.int32), rng.permutation(num_pages).astype(np.int32)[:9]
+    table, parents = rng.permutation(num_pages)[:B * most].astype(np.int32).reshape(B, most), np.stack([R.random_parents(rng, n) for _ in range(B)])
+    given = [cache, new, parents, free, np.array([9], np.int32), held, table]
+    sizes = [x.size for x in given] + [B, B, B * n, B * n, 2 * B * n, 1, B]
+    buf = torch.full((sum(sizes) + 2,), -77, dtype=I32, device=gpu_device)
+    odd = (sum(sizes[:11]) + 1) % 2                   # (the masks' place has to be a multiple of 8 bytes)
+    parts = list(buf[1 - odd:1 - odd + sum(sizes)].split(sizes))
+    for t, x in zip(parts, given):
+        t.copy_(torch.from_numpy(x.reshape(-1)))
+    c, w, p, f, k, h, t, granted, seqlens, pos, slots, masks, left, after = parts
+    loza.loza_ssa_step_tables(c, w, p.view(B, n), f, k, t.view(B, most), num_pages, page, granted, seqlens, pos.view(B, n), slots.view(B, n),
+                              masks.view(torch.int64).view(B, n), left, held=h, held_after=after)
+    torch.cuda.synchronize()
+    ref = step_tables_held(cache, new, parents, free, 9, held, table, n, num_pages, page)
+    got = (granted, seqlens, pos, slots, masks.view(torch.int64), left, t, after)
+    for g, r in zip(got, ref):
+        assert np.array_equal(g.cpu().numpy(), r.reshape(-1))
+    for g, x in zip(parts, given[:6]):
+        assert np.array_equal(g.cpu().numpy(), x.reshape(-1))
+    assert int(buf[-1]) == -77 and (odd == 1 or int(buf[0]) == -77)

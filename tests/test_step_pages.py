@@ -41,3 +41,29 @@ def test_the_definition_loses_no_page(B_, n, page, most, pages, tree):
     for _ in range(300):
         pool.step(n, tree)
     assert pool.ended > 3                              # (far beyond what the pool holds once)
+
+
+@pytest.mark.parametrize("held", [True, False])
+def test_no_result_may_lie_on_another_array(held):
+    """Workgroups read what others write: requests would get the same page. (Refused before anything is launched.)"""
+    B_, n, most = 2, 8, 16
+    sizes = dict(granted=4 * B_, seqlens=4 * B_, pos=4 * B_ * n, slots=4 * B_ * n, masks=8 * B_ * n, left=4, after=4 * B_, table=4 * B_ * most,
+                 cache=4 * B_, new=4 * B_, parents=4 * B_ * n, free=40, count=4, held=4 * B_)
+    results = ["granted", "seqlens", "pos", "slots", "masks", "left", "table"] + (["after"] if held else [])
+    at = dict(cache=1, new=2, parents=3, free=4, count=5, held=13, table=6, granted=7, seqlens=8, pos=9, slots=10, masks=11, left=12, after=14)
+
+    def call(**k):
+        if held:
+            return _held(**k)
+        a = dict(cache=A, new=2 * A, parents=3 * A, free=4 * A, count=5 * A, table=6 * A, B=2, n=8, num_free=10, num_pages=100, page=64, most=16,
+                 granted=7 * A, seqlens=8 * A, pos=9 * A, slots=10 * A, masks=11 * A, left=12 * A)
+        a.update(k)
+        return B.lib().loza_ssa_step_tables(*a.values(), None)
+    for r in results:
+        for other in sizes:
+            if other == r or (not held and other in ("held", "after")):
+                continue
+            step = 8 if r == "masks" else 4
+            assert call(**{r: at[other] * A}) == ERR_SHAPE, (r, other)
+            assert call(**{r: at[other] * A + (sizes[other] - 4) // step * step}) == ERR_SHAPE, (r, other)        # its last word
+            assert call(**{r: at[other] * A - (sizes[r] - 1) // step * step}) == ERR_SHAPE, (r, other)            # this one's last word
