@@ -170,8 +170,23 @@ hipError_t launch_rope(const RopeParams &p, int elem_bytes, hipStream_t stream)
     };
     const bool wide = heads(p.q) && heads(p.k) && whole(p.interleaved ? p.rot : p.rot / 2) &&
                       (p.v == nullptr || (at16(p.v) && at16(p.v_rows) && whole(p.v_token) && whole(p.v_head) && whole(p.d_v)));
-    if (elem_bytes == 2) return wide ? launch_v<uint16_t, 8>(p, stream) : launch_v<uint16_t, 1>(p, stream);
-    return wide ? launch_v<float, 4>(p, stream) : launch_v<float, 1>(p, stream);
+    // (a launch has fewer than 2^32 threads in x: 2^23 workgroups at most for these tokens, and calls of more in parts)
+    constexpr int64_t kMostTokens = 1 << 24;
+    RopeParams part = p;
+    for (int64_t t0 = 0; t0 < p.T; t0 += kMostTokens) {
+        auto from = [&](const void *x, int64_t token) { return x ? (const char *)x + t0 * token * elem_bytes : nullptr; };
+        part.T = p.T - t0 < kMostTokens ? p.T - t0 : kMostTokens;
+        part.q.x = from(p.q.x, p.q.x_token);
+        part.q.out = (void *)from(p.q.out, p.q.out_token);
+        part.k.x = from(p.k.x, p.k.x_token);                          // (rows of the cache are by slot)
+        part.v = from(p.v, p.v_token);
+        part.positions = p.positions + t0;
+        part.slots = p.slots ? p.slots + t0 : nullptr;
+        const hipError_t e = elem_bytes == 2 ? (wide ? launch_v<uint16_t, 8>(part, stream) : launch_v<uint16_t, 1>(part, stream))
+                                             : (wide ? launch_v<float, 4>(part, stream) : launch_v<float, 1>(part, stream));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace loza

@@ -1,0 +1,31 @@
+"""Calls of more tokens, or more sequences, than one launch takes (its threads in x are fewer than 2^32)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_23966_amd as loza
+
+pytestmark = pytest.mark.gpu
+BF, I32 = torch.bfloat16, torch.int32
+
+
+@pytest.mark.parametrize("append", [False, True])
+def test_rope_of_more_tokens_than_a_launch_takes(gpu_device, append):
+    """2^25 + 3 tokens of one narrow head, a thousand rows and positions over and over, against a call of those."""
+    T, d = (1 << 25) + 3, 4
+    freq = loza.loza_ssa_rope_frequencies(2, 10000.0)[0].to(gpu_device)
+    pos = (torch.arange(T, device=gpu_device) % 1000).to(I32)
+    pos[12345::1 << 20] = -1
+    x = torch.randn(1000, 1, d, generator=torch.Generator(device=gpu_device).manual_seed(1), device=gpu_device).to(BF)
+    rows = torch.arange(T, device=gpu_device) % 1000
+    y = torch.full((T, 1, d), 7.0, dtype=BF, device=gpu_device)
+    if append:
+        slots = torch.arange(T - 1, -1, -1, device=gpu_device).to(I32)
+        loza.loza_ssa_rope_append(None, x[rows], None, pos, slots, freq, None, y, None, 0, 2, True)
+        y = y.flip(0)
+    else:
+        loza.loza_ssa_rope(x[rows], pos, freq, y, 2, True)
+    small = torch.full_like(x, 7.0)
+    loza.loza_ssa_rope(x, torch.arange(1000, dtype=I32, device=gpu_device), freq, small, 2, True)
+    want = torch.where((pos >= 0)[:, None, None], small[rows], torch.tensor(7.0, dtype=BF, device=gpu_device))
+    assert torch.equal(y, want)
