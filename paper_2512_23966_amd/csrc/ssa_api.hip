@@ -58,6 +58,13 @@ int check_common(int B, int Hq, int Hkv, int64_t S, int d_qk, int d_v, int64_t n
     return LOZA_OK;
 }
 
+// A launch of `tiles` workgroups of each (batch, key head). (Step by step: the product of all may pass 64 bits.)
+bool launch_fits(int64_t tiles, int Hkv, int B, int threads = 256)
+{
+    const int64_t most = loza::most_workgroups(threads);
+    return tiles <= most && tiles * Hkv <= most && tiles * Hkv * B <= most;
+}
+
 // LOZA_DECODE_SPLITS (documented in the header): another split count, for tests and experiments; 0: none given
 int forced_splits()
 {
@@ -394,6 +401,15 @@ static size_t tree_bytes(int B, int Hq, int Hkv, int64_t n, int d_v, const TreeP
     return (size_t)(loza::tree_part_floats(blocks, plan.n_splits, d_v) + blocks * plan.n_splits * 96) * sizeof(float);
 }
 
+// Sizes of a tree call beyond check_common's: its nodes, and as many tiles as a launch takes (width 128: tiles of 256 rows, by 512 threads)
+static int check_tree(int B, int Hq, int Hkv, int64_t S, int n, int d_qk)
+{
+    if (n < 1 || n > S || n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
+    const int64_t rows = (int64_t)n * (Hq / Hkv);
+    const bool fits = d_qk > 128 ? launch_fits((rows + loza::kTileRows - 1) / loza::kTileRows, Hkv, B) : launch_fits((rows + 255) / 256, Hkv, B, 512);
+    return fits ? LOZA_OK : LOZA_ERR_SHAPE;
+}
+
 static int prefill_bf16(const void *q, const void *k, const void *v, void *out, float *lse,
                         int B, int Hq, int Hkv, int64_t S, int d_qk, int d_v,
                         int64_t sink, int64_t local, int64_t block, bool blocks, float scale, void *stream,
@@ -423,7 +439,9 @@ static int prefill_bf16(const void *q, const void *k, const void *v, void *out, 
     const int G = Hq / Hkv;
     const int rows = loza::prefill_rows_per_tile();
     const int64_t row_tiles = ((extend ? q_len : S) * G + rows - 1) / rows;
-    if (row_tiles * Hkv * B > 2147483647LL) return LOZA_ERR_SHAPE;
+    // (tiles of 128 rows, or, width 128 and more than one of these, of 256 by 512 threads)
+    if (!launch_fits(row_tiles, Hkv, B) || (d_qk == 128 && row_tiles > 1 && !launch_fits((row_tiles + 1) / 2, Hkv, B, 512))) return LOZA_ERR_SHAPE;
+    if (tree_masks) { if (int rc = check_tree(B, Hq, Hkv, S, (int)q_len, d_qk)) return rc; }
     if (validate_only) return LOZA_OK;
 
     loza::FwdParams p{};
@@ -892,9 +910,9 @@ static int backward_fill(loza::BwdParams &p, int B, int Hq, int Hkv, int64_t S, 
     backward_plan(p);
     const int64_t n_kt = (S + 63) / 64;
     const int64_t items = (int64_t)p.n_sink_kt * p.max_chunks + (n_kt - p.n_sink_kt);
-    if (items * Hkv * B > 2147483647LL || ((S * p.G + 63) / 64) * Hkv * B > 2147483647LL ||
-        ((int64_t)B * S * Hq + 3) / 4 > 2147483647LL)
-        return LOZA_ERR_SHAPE;
+    if (!launch_fits(items, Hkv, B) || !launch_fits((S * p.G + 63) / 64, Hkv, B)) return LOZA_ERR_SHAPE;
+    // (the sums of sinks whose rows are split: 1,024 columns a workgroup, of 64 keys a tile; keys that are split to fill the chip are few)
+    if (p.max_chunks > 1 && !launch_fits((int64_t)p.n_sink_kt * (alias ? d_qk : d_qk + d_v) / 16, Hkv, B)) return LOZA_ERR_SHAPE;
     return LOZA_OK;
 }
 
@@ -1096,7 +1114,9 @@ static int decode_bf16(const void *q, const void *kcache, const void *vcache, co
     const DecodePlan plan = decode_plan(B, Hq, Hkv, S_max, d_qk, n_sink, window);
     const int n_splits = plan.n_splits;
     const int64_t row_tiles = (G + rows - 1) / rows;
-    if (row_tiles * Hkv * B * decode_splits(B, Hq, Hkv, S_max, n_sink, window) > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (!launch_fits((plan.rows ? (G + 15) / 16 : row_tiles) * n_splits, Hkv, B)) return LOZA_ERR_SHAPE;
+    // the merges: a workgroup of d_v / 4 threads a query, or one of 256 for 128 of its columns
+    if (!plan.rows ? !launch_fits(G, Hkv, B, d_v / 4) : n_splits > 1 && !launch_fits((int64_t)G * (d_v / 128), Hkv, B)) return LOZA_ERR_SHAPE;
 
     loza::FwdParams p{};
     p.q = (const uint16_t *)q; p.k = (const uint16_t *)kcache; p.v = (const uint16_t *)vcache;
@@ -1193,18 +1213,11 @@ int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int3
                         tree_lens, masks);
 }
 
-// Sizes of a tree call beyond check_common's: its nodes, and as many tiles as a launch takes (as prefill_bf16 counts them)
-static int check_tree(int B, int Hq, int Hkv, int64_t S, int n)
-{
-    if (n < 1 || n > S || n > LOZA_TREE_MAX_NODES) return LOZA_ERR_SHAPE;
-    return ((int64_t)n * (Hq / Hkv) + loza::kTileRows - 1) / loza::kTileRows * Hkv * B > 2147483647LL ? LOZA_ERR_SHAPE : LOZA_OK;
-}
-
 size_t loza_ssa_extend_tree_workspace_bytes(int B, int Hq, int Hkv, int64_t S_max, int n, int d_qk, int d_v,
                                             int64_t sink_blocks, int64_t local_blocks, int64_t block)
 {
     if (check_common(B, Hq, Hkv, S_max, d_qk, d_v, sink_blocks, local_blocks, 1.0f) != LOZA_OK) return 0;
-    if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || check_tree(B, Hq, Hkv, S_max, n) != LOZA_OK) return 0;
+    if (check_blocks(sink_blocks, local_blocks, block) != LOZA_OK || check_tree(B, Hq, Hkv, S_max, n, d_qk) != LOZA_OK) return 0;
     if (!loza::bf16_shape_supported(d_qk, d_v, true)) return 0;
     return tree_bytes(B, Hq, Hkv, n, d_v, tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), true));
 }
@@ -1214,7 +1227,7 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
 {
     if (int rc = check_common(B, Hq, Hkv, S_max, d_qk, 1, sink_blocks, local_blocks, 1.0f)) return rc;
     if (int rc = check_blocks(sink_blocks, local_blocks, block)) return rc;
-    if (int rc = check_tree(B, Hq, Hkv, S_max, n)) return rc;
+    if (int rc = check_tree(B, Hq, Hkv, S_max, n, d_qk)) return rc;
     if (!loza::bf16_width_supported(d_qk)) return LOZA_ERR_UNSUPPORTED;
     const TreePlan plan = tree_plan(B, Hkv, Hq / Hkv, n, S_max, d_qk, block_pattern(sink_blocks, local_blocks, block, S_max), scratch != 0);
     if (n_splits) *n_splits = plan.n_splits;

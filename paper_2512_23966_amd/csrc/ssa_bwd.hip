@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256) void ssa_bwd_rowstat_kernel(const BwdParams p)
 {
     constexpr int LPR = DV / 8 < 64 ? DV / 8 : 64;                     // lanes per row, 16 bytes each
     const int lane = threadIdx.x % LPR;
-    const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;  // flat (b, i, h)
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;  // flat (b, i, h)
     const int64_t n_rows = (int64_t)p.B * p.S * p.Hq;
     if (row >= n_rows) return;
     const uint16_t *o = p.out + row * DV, *d = p.dout + row * DV;
@@ -669,7 +669,8 @@ static hipError_t launch_backward_t(const BwdParams &p, const WidePlan *wide, hi
 {
     const int64_t n_rows = (int64_t)p.B * p.S * p.Hq;
     constexpr int RPB = 256 / (DV / 8 < 64 ? DV / 8 : 64);             // rows per workgroup
-    hipLaunchKernelGGL((ssa_bwd_rowstat_kernel<DV>), dim3((unsigned)((n_rows + RPB - 1) / RPB)), dim3(256), 0, stream, p);
+    const int64_t stat = (n_rows + RPB - 1) / RPB, gx = stat < (1 << 22) ? stat : (1 << 22), gy = (stat + gx - 1) / gx;   // (most_workgroups)
+    hipLaunchKernelGGL((ssa_bwd_rowstat_kernel<DV>), dim3((unsigned)gx, (unsigned)gy), dim3(256), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (wide) return launch_bwd_wide(p, *wide, stream);

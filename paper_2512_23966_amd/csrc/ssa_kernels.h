@@ -44,6 +44,9 @@ struct FwdParams {
     const int64_t *tree_masks;
 };
 
+// Workgroups that a launch takes in x: fewer than 2^32 threads. (One of more comes back without an error, and the work beyond is left out.)
+constexpr int64_t most_workgroups(int threads) { return 0xffffffffLL / threads; }
+
 // The tile kernels use more dynamic LDS than the default limit: raised once per kernel and device.
 template <auto KERN>
 static hipError_t allow_lds(int bytes)
