@@ -358,7 +358,7 @@ __global__ __launch_bounds__(64 * F32_WAVES) void ssa_backward_f32_dq_kernel(con
     __shared__ float s_q[F32_WAVES][F32_MAX_D], s_do[F32_WAVES][F32_MAX_D];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t n_rows = (int64_t)p.B * p.S * p.Hq;
-    const int64_t r = (int64_t)blockIdx.x * F32_WAVES + wave;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * F32_WAVES + wave;
     if (r >= n_rows) return;  // whole wavefront leaves together; no block-wide barrier is used
     const int h = (int)(r % p.Hq);
     const int64_t bi = r / p.Hq;
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(64 * F32_WAVES) void ssa_backward_f32_dkv_kernel(co
     __shared__ float s_k[F32_WAVES][F32_MAX_D], s_v[F32_WAVES][F32_MAX_D];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t n_keys = (int64_t)p.B * p.S * p.Hkv;
-    const int64_t kr_idx = (int64_t)blockIdx.x * F32_WAVES + wave;  // flat (b, j, g)
+    const int64_t kr_idx = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * F32_WAVES + wave;  // flat (b, j, g)
     if (kr_idx >= n_keys) return;
     const int g = (int)(kr_idx % p.Hkv);
     const int64_t bj = kr_idx / p.Hkv;
@@ -496,12 +496,15 @@ __global__ __launch_bounds__(64 * F32_WAVES) void ssa_backward_f32_dkv_kernel(co
 hipError_t launch_backward_f32(const F32BwdParams &p, hipStream_t stream)
 {
     const int64_t n_rows = (int64_t)p.B * p.S * p.Hq, n_keys = (int64_t)p.B * p.S * p.Hkv;
-    hipLaunchKernelGGL(ssa_backward_f32_dq_kernel, dim3((unsigned)((n_rows + F32_WAVES - 1) / F32_WAVES)), dim3(64 * F32_WAVES), 0,
-                       stream, p);
+    // (a grid row holds fewer than 2^32 threads)
+    auto grid = [](int64_t waves) {
+        const int64_t blocks = (waves + F32_WAVES - 1) / F32_WAVES, gx = blocks < (1 << 22) ? blocks : (1 << 22);
+        return dim3((unsigned)gx, (unsigned)((blocks + gx - 1) / gx));
+    };
+    hipLaunchKernelGGL(ssa_backward_f32_dq_kernel, grid(n_rows), dim3(64 * F32_WAVES), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(ssa_backward_f32_dkv_kernel, dim3((unsigned)((n_keys + F32_WAVES - 1) / F32_WAVES)), dim3(64 * F32_WAVES), 0,
-                       stream, p);
+    hipLaunchKernelGGL(ssa_backward_f32_dkv_kernel, grid(n_keys), dim3(64 * F32_WAVES), 0, stream, p);
     return hipGetLastError();
 }
 

@@ -29,3 +29,20 @@ def test_rope_of_more_tokens_than_a_launch_takes(gpu_device, append):
     loza.loza_ssa_rope(x, torch.arange(1000, dtype=I32, device=gpu_device), freq, small, 2, True)
     want = torch.where((pos >= 0)[:, None, None], small[rows], torch.tensor(7.0, dtype=BF, device=gpu_device))
     assert torch.equal(y, want)
+
+
+def test_f32_backward_of_more_rows_than_a_launch_takes(gpu_device):
+    """2^26 + 48 rows (a wave each): 200 short sequences over and over, against a call of those."""
+    b, S, H, d, many = 200, 4, 4, 4, (1 << 22) + 3
+    g = torch.Generator(device=gpu_device).manual_seed(3)
+    r = lambda *s: torch.randn(*s, generator=g, device=gpu_device)
+    q, k, v, dout = (r(b, S, H, d) for _ in range(4))
+    out, lse = torch.empty_like(q), torch.empty(b, H, S, device=gpu_device)
+    loza.loza_ssa_prefill_f32(q, k, v, out, lse, 1, 2, 0.5)
+    small = [torch.empty_like(q) for _ in range(3)]
+    loza.loza_ssa_backward_f32(q, k, v, out, lse, dout, *small, 1, 2, 0.5)
+    at = torch.arange(many, device=gpu_device) % b
+    got = [torch.full((many, S, H, d), float("nan"), device=gpu_device) for _ in range(3)]
+    loza.loza_ssa_backward_f32(q[at], k[at], v[at], out[at], lse[at], dout[at], *got, 1, 2, 0.5)
+    for x, y in zip(got, small):
+        assert torch.equal(x, y[at])
