@@ -585,6 +585,7 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
  *   path [B, n] int32: nodes on the path, node 0 first, then -1     path_lens [B] int32: how many (0 for an empty tree)
  *   next_token [B] int32: the token after the path; -1 for an empty tree or a target row without weight
  *   workspace: loza_ssa_verify_tree_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
+ * A token whose target probability is negative or a NaN, or whose draft probability is a NaN, weighs 0. Infinite ones are not allowed.
  * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30. Sums and decisions in fp64, always in the same order.
  */
 int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,

@@ -212,7 +212,7 @@ __device__ __forceinline__ bool walk_on(Walk &w)
             a = p - w.c * q;
             a = a > 0 ? a : 0;
         } else {
-            a = (__ballot(w.token == lane_value(w.token, r)) & w.gone) ? 0 : p;
+            a = !(p > 0) || (__ballot(w.token == lane_value(w.token, r)) & w.gone) ? 0 : p;
         }
         w.last = r;
         if (u * q * w.s < a) {
@@ -231,7 +231,7 @@ __device__ __forceinline__ bool walk_on(Walk &w)
     }
 }
 
-// The residual weights at a node: what a token's weight is, given its probabilities.
+// The residual weights at a node: what a token's weight is, given its probabilities; 0 where one of them is a NaN, or the target's is negative.
 template <bool DRAFT>
 struct Residual {
     const float *p, *q;
@@ -255,7 +255,7 @@ struct Residual {
             return a > 0 ? a : 0;
         } else {
             for (uint64_t g = gone; g; g &= g - 1) px = x == lane_value(token, __builtin_ctzll(g)) ? 0.f : px;
-            return px;
+            return __builtin_amdgcn_fmed3f(px, 0.f, __builtin_inff());   // (of a NaN: the least of the others)
         }
     }
     __device__ __forceinline__ double at(int x) const { return weight(x, p[x], DRAFT ? q[x] : 0.f); }
