@@ -556,8 +556,12 @@ int loza_ssa_rope_frequencies(int rot_dim, double base, double factor, int64_t o
  *           i = P + popcount(mask) - 1 and sees cache row j < P if j is live for position i, and the node of
  *           the k-th set bit (from 0) if position P + k is. A chain's masks (bits 0 .. r) give what loza_ssa_extend
  *           gives. A mask of 0: the row sees nothing, out = 0, lse = -inf, whatever its query holds.
- *   pattern, supported shapes, numerics: as loza_ssa_extend_blocks (block = 1: token-granular)
- *   workspace: as loza_ssa_extend_with_workspace, loza_ssa_extend_tree_workspace_bytes of it; NULL: no workgroups share keys
+ *   pattern, supported shapes, numerics: as loza_ssa_extend_blocks (block = 1: token-granular); where workgroups share keys, weights of two terms
+ *   workspace: loza_ssa_extend_tree_workspace_bytes (S_max = max_pages_per_seq * page_size of a paged cache; 0: these sizes need none), 16-byte
+ *           aligned, left alone until the launches have run, contents ignored. A smaller one is LOZA_ERR_WORKSPACE (loza_ssa_extend_with_workspace
+ *           takes some that are: sizes that callers of it may have kept). NULL: no workgroups share keys; slower, and other bits
+ * As many sequences and heads as a launch takes: n Hq / Hkv rows make tiles of 128 (width 128: of 256); of all key heads and sequences fewer than 2^24 (2^23),
+ * else LOZA_ERR_SHAPE.
  */
 int loza_ssa_extend_tree(const void *q, const void *k, const void *v, const int32_t *block_table, const int32_t *seqlens,
                          const int32_t *tree_lens, const int64_t *masks, void *out, float *lse, int B, int Hq, int Hkv,

@@ -226,7 +226,7 @@ ExtendPlan extend_plan(int B, int Hkv, int G, int64_t q_len, int64_t S, int d_qk
 
 // Which kernel takes a tree of drafted tokens, how many workgroups share the keys of a row (1 without scratch memory), and whether tiles that are
 // not split take two-term weights from the outset. A time model in microseconds, like extend_plan's, fitted to 250 sizes of 1 to 16 sequences and
-// 2 to 64 nodes; a tree has at most 64 nodes, so most calls leave the chip idle unless keys are shared, and calls that the few-rows kernel
+// 2 to 64 nodes (larger batches are extrapolated); a tree has at most 64 nodes, so most calls leave the chip idle unless keys are shared, and calls that the few-rows kernel
 // takes in one full round are not left to it (window 8192, wide: one sequence of 33 nodes 153 us, its tiles in 15 parts 78; 8 of 8 nodes 156, in 8 113).
 // Width 128 has the few-rows kernel and tiles of 256 rows, split or not; a tile that is mostly padding costs less (8 key heads, window 4096,
 // 8 sequences of 37 nodes: 128-row tiles in 4 parts 88 us, 256-row tiles in 4 parts 52).

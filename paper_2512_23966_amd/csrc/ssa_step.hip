@@ -55,7 +55,7 @@ __device__ __forceinline__ Request request_of(const TablesParams &p, int b)
 
 // A workgroup takes kTokens tokens of one request. Pages are dealt out in the order of the requests, so each workgroup adds up what the
 // requests before its own take (a scan across workgroups would cost a launch; 512 requests read 2 KB each, out of L2). Bound by the latency
-// of four loads that wait for each other: 16 trees of 64 nodes 3.6 us, 512 requests of 200 tokens 6.2.
+// of four loads that wait for each other: 16 trees of 64 nodes 3.7 us, 512 requests of 200 tokens 6.1.
 constexpr int kTokens = 1024;
 
 __global__ __launch_bounds__(256) void step_tables_kernel(const TablesParams p)
@@ -483,7 +483,8 @@ hipError_t launch_step_tables(const TablesParams &p, hipStream_t stream)
 // sum of calls whose probabilities are still in a cache when they are small enough for one (32,000 tokens, one chain of 5 nodes: 9.1 us, with a round 10.7;
 // from memory 16.7 and 14.6). A chain or drafts that are not random need one sum (131,072 tokens from memory, 16 sequences of 5 nodes: no round 36.8 us,
 // one 20.0, two 23.2); wider trees of random drafts need as many as children are rejected (16 of 16 nodes: one round 44 us, three 33,
-// four 37; one of 64: one 31, three 23, five 30; 16 of 64: one 99, three 81, five 65, six 61, eight 73).
+// four 37; one of 64: one 31, three 23, five 30; 16 of 64: one 99, three 81, five 65, six 61, eight 73). Measured on up to 16 trees; from some 64
+// on slices are few (16 of 64 trees, 2 of 512), and a sum beyond the rounds, taken by one wave a slice, leaves most of its workgroup idle.
 void verify_plan(VerifyParams &p, bool draft)
 {
     int64_t slices = (1024 + p.B - 1) / p.B;
