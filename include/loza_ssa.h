@@ -447,9 +447,10 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  * Pages. A page belongs to the request whose row of block_table names it until the engine puts it back on the free list, also where it holds nothing but rows
  * that were not kept. Chunks keep all their rows; a step of drafts keeps a part of them, and leaves a request with more pages than its cache_len
  * needs: loza_ssa_step_tables_held is told how many, and deals out new ones behind those (with loza_ssa_step_tables the engine has to put
- * the pages [ceil((cache_len + path_len) / page_size), ceil(seqlen / page_size)) of each row back itself, or they are lost). Between two steps:
- * cache_lens += path_lens, free_count = free_left, held = held_after. A request that ends has the first `held` entries of its row appended to
- * free_pages at free_count, and cache_len = held = 0.
+ * the pages [ceil((cache_len + path_len) / page_size), ceil(seqlen / page_size)) of each row back itself, or they are lost). An engine whose requests
+ * take both, chunks and drafts, tells it with both. Between two steps: cache_lens += path_lens (chunks: granted), free_count = free_left, held = held_after.
+ * A request that ends has the first `held` entries of its row appended to free_pages from free_count on (which has room for every page), free_count grows by
+ * as many, and its cache_len and held are 0.
  */
 #define LOZA_TREE_MAX_NODES 64
 #define LOZA_ROPE_MAX_DIM 1024
@@ -589,7 +590,7 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
  *   path [B, n] int32: nodes on the path, node 0 first, then -1     path_lens [B] int32: how many (0 for an empty tree)
  *   next_token [B] int32: the token after the path; -1 for an empty tree or a target row without weight
  *   workspace: loza_ssa_verify_tree_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
- * A token whose target probability is negative or a NaN, or whose draft probability is a NaN, weighs 0. Infinite ones are not allowed.
+ * A token whose target probability is negative or a NaN, or whose draft probability is a NaN, weighs 0. Infinite probabilities, and negative ones of the draft, are not allowed.
  * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30. Sums and decisions in fp64, always in the same order.
  */
 int loza_ssa_verify_tree(const float *target, const float *draft, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,

@@ -1,7 +1,9 @@
 """The pages of a step whose rows are not all kept: the definition (plain integers) keeps every page, and the call's refusals. No GPU needed."""
 import numpy as np
 import pytest
+import torch
 
+import paper_2512_23966_amd as loza
 from paper_2512_23966_amd import binding as B
 from tests import step_reference as R
 from tests.step_pages import Pool, step_tables_held
@@ -67,3 +69,13 @@ def test_no_result_may_lie_on_another_array(held):
             assert call(**{r: at[other] * A}) == ERR_SHAPE, (r, other)
             assert call(**{r: at[other] * A + (sizes[other] - 4) // step * step}) == ERR_SHAPE, (r, other)        # its last word
             assert call(**{r: at[other] * A - (sizes[r] - 1) // step * step}) == ERR_SHAPE, (r, other)            # this one's last word
+
+
+def test_binding_takes_both_counts_or_none():
+    z = torch.zeros(2, 4, dtype=torch.int32)
+    args = (z[:, 0], z[:, 0], None, z[0], z[0, :1], z, 4, 64, z[:, 0], z[:, 0], z, z, None, z[0, :1])
+    for one in (dict(held=z[:, 0]), dict(held_after=z[:, 0])):
+        with pytest.raises(ValueError):
+            loza.loza_ssa_step_tables(*args, **one)
+    with pytest.raises(TypeError):
+        loza.loza_ssa_step_tables(*args, held=z[:, 0], held_after=z[:, 0])
