@@ -46,3 +46,21 @@ def test_f32_backward_of_more_rows_than_a_launch_takes(gpu_device):
     loza.loza_ssa_backward_f32(q[at], k[at], v[at], out[at], lse[at], dout[at], *got, 1, 2, 0.5)
     for x, y in zip(got, small):
         assert torch.equal(x, y[at])
+
+
+@pytest.mark.parametrize("inter", [True, False])
+def test_rope_in_place_across_launches(gpu_device, inter):
+    """2^24 + 5 tokens with 16-byte rows, out of place into wider rows and in place."""
+    T, d = (1 << 24) + 5, 16
+    freq = loza.loza_ssa_rope_frequencies(d, 10000.0)[0].to(gpu_device)
+    at = torch.arange(T, device=gpu_device) % 1000
+    pos = at.to(I32)
+    x = torch.randn(1000, 1, d, generator=torch.Generator(device=gpu_device).manual_seed(2), device=gpu_device).to(BF)
+    small = torch.empty_like(x)
+    loza.loza_ssa_rope(x, torch.arange(1000, dtype=I32, device=gpu_device), freq, small, 0, inter)
+    y = x[at]
+    wide = torch.full((T, 1, d + 8), 7.0, dtype=BF, device=gpu_device)
+    loza.loza_ssa_rope(y, pos, freq, wide[..., 8:], 0, inter)
+    assert torch.equal(wide[..., 8:], small[at]) and bool((wide[..., :8] == 7).all())
+    loza.loza_ssa_rope(y, pos, freq, y, 0, inter)
+    assert torch.equal(y, small[at])
