@@ -534,6 +534,57 @@ int loza_ssa_rope_append_f32(const float *q, const float *k, const float *v, con
                              int interleaved, float mscale, void *stream);
 
 /*
+ * Norms of heads with their rotary positions, in one pass. Over the columns [norm_begin, norm_begin + norm_dim) of a head, with
+ * r = (mean of x_c^2 + eps)^(-1/2): y_c = x_c r weight_c; elsewhere y_c = x_c; then the columns [rot_begin, rot_begin + rot_dim) of y are rotated as
+ * loza_ssa_rope rotates them. The two ranges may be apart (a latent row: 512 normed columns, 64 rotated ones), the same (heads of width 128), or overlap.
+ *   weight [norm_dim] fp32, NULL: ones     1 <= norm_dim, d <= LOZA_NORM_MAX_DIM; eps: a positive normal number
+ *   everything else, padding, strides and in-place calls among it: as loza_ssa_rope. A head whose squares add up to more than fp32 holds gives 0.
+ * Sums in fp32, one rounding of each result. Arrays of which x and out are slices may differ; all heads have the one weight.
+ */
+#define LOZA_NORM_MAX_DIM 1024
+int loza_ssa_norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                       int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
+                       int rot_begin, int rot_dim, int interleaved, float mscale, void *stream);
+int loza_ssa_norm_rope_f32(const float *x, const float *weight, const int32_t *positions, const double *freq, float *out, int64_t T, int H, int d,
+                           int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
+                           int rot_begin, int rot_dim, int interleaved, float mscale, void *stream);
+
+/*
+ * Its gradient: with g the rotation of dout by the negative angles (times mscale), and h = g weight on the norm columns,
+ *     dx_c = r (h_c - x_c r^2 mean(h x)) there, g_c elsewhere;     dweight_c = sum over tokens and heads of g_c x_c r.
+ *   x: what the forward call was given (not its result)     dx [T, H, d]: strided; dx == dout or dx == x with the same strides: in place. The row of a
+ *           token with a negative position is left as it is, and adds nothing to dweight
+ *   dweight [norm_dim] fp32, overwritten; NULL: not wanted, and no workspace is needed
+ *   workspace: loza_ssa_norm_rope_backward_workspace_bytes, 16-byte aligned, contents ignored; two calls that overlap in time need two
+ * dweight's sums run in an order that depends on the sizes and the alignment alone, in fp32 within and in fp64 across workgroups.
+ */
+size_t loza_ssa_norm_rope_backward_workspace_bytes(int64_t T, int H, int d, int norm_dim);
+int loza_ssa_norm_rope_backward(const void *dout, const void *x, const float *weight, const int32_t *positions, const double *freq, void *dx,
+                                float *dweight, int64_t T, int H, int d, int64_t dout_token, int64_t dout_head, int64_t x_token, int64_t x_head,
+                                int64_t dx_token, int64_t dx_head, int norm_begin, int norm_dim, float eps, int rot_begin, int rot_dim,
+                                int interleaved, float mscale, void *workspace, size_t workspace_bytes, void *stream);
+int loza_ssa_norm_rope_backward_f32(const float *dout, const float *x, const float *weight, const int32_t *positions, const double *freq, float *dx,
+                                    float *dweight, int64_t T, int H, int d, int64_t dout_token, int64_t dout_head, int64_t x_token, int64_t x_head,
+                                    int64_t dx_token, int64_t dx_head, int norm_begin, int norm_dim, float eps, int rot_begin, int rot_dim,
+                                    int interleaved, float mscale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * loza_ssa_rope_append with those norms: queries and keys are normed and rotated (q_norm_dim or k_norm_dim 0: not normed, the weight unused), keys
+ * and values go to the cache in the same launch. d_q, d_k <= LOZA_NORM_MAX_DIM; everything else as loza_ssa_rope_append.
+ */
+int loza_ssa_norm_rope_append(const void *q, const float *q_weight, const void *k, const float *k_weight, const void *v, const int32_t *positions,
+                              const int32_t *slots, const double *freq, void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q,
+                              int d_k, int d_v, int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token,
+                              int64_t k_head, int64_t v_token, int64_t v_head, int64_t cache_rows, int q_norm_begin, int q_norm_dim, int k_norm_begin,
+                              int k_norm_dim, float eps, int q_rot_begin, int k_rot_begin, int rot_dim, int interleaved, float mscale, void *stream);
+int loza_ssa_norm_rope_append_f32(const float *q, const float *q_weight, const float *k, const float *k_weight, const float *v, const int32_t *positions,
+                                  const int32_t *slots, const double *freq, float *q_out, float *k_rows, float *v_rows, int64_t T, int Hq, int Hkv,
+                                  int d_q, int d_k, int d_v, int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token,
+                                  int64_t k_head, int64_t v_token, int64_t v_head, int64_t cache_rows, int q_norm_begin, int q_norm_dim,
+                                  int k_norm_begin, int k_norm_dim, float eps, int q_rot_begin, int k_rot_begin, int rot_dim, int interleaved,
+                                  float mscale, void *stream);
+
+/*
  * Host-only (ours). Frequencies for contexts stretched by `factor` (the paper's YaRN, Training section): f_k = base^(-2k / rot_dim)
  * turns original_context * f_k / 2 pi times over the context that was trained; pairs of fewer than slow_turns (usually 1) are divided by the
  * factor, pairs of more than fast_turns (usually 32) are kept, those between are mixed linearly in their turns.
@@ -606,6 +657,99 @@ size_t loza_ssa_verify_tree_workspace_bytes(int B, int n, int V);
  */
 int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, const int32_t *path, const int32_t *path_lens, int B, int n,
                            int n_layers, int64_t cache_rows, int64_t k_row_bytes, int64_t v_row_bytes, void *stream);
+
+/*
+ * What loza_ssa_verify_tree takes as `target` (or `draft`), from logits: penalties for repeated tokens, biases, grammar masks, temperature, softmax.
+ *   logits [B, n] rows of V, logits_row >= V elements apart (bf16 or fp32)     probs [B, n, V] fp32; the fp32 call: probs == logits with logits_row == V in place
+ *   tree_lens [B] int32 or NULL (n rows each): rows r >= tree_lens[b] of probs are left as they are, and their logits are not read
+ *   tokens [B, n] int32, masks [B, n] int64, or both NULL: a row's own path (loza_ssa_step_tables makes the masks): the tokens of the nodes in masks[b, r],
+ *           those below tree_lens[b], were said as well, each once a node
+ *   seen [B] rows, seen_row elements apart (a multiple of 8, >= V; 16-byte aligned), or NULL: what was said before the path (loza_ssa_count_tokens):
+ *           bit 15 says that the token occurs in the prompt, the others how often it was said
+ *   repetition (> 0; NULL: 1), frequency, presence (NULL: 0), temperature (NULL: 1) [B] fp32
+ *   bias_tokens [B, n_bias] int32, bias_values [B, n_bias] fp32 (n_bias <= LOZA_MAX_BIAS; tokens outside [0, V) are skipped, those of one token add up in order)
+ *   allowed [B, n, ceil(V / 32)] int32 or NULL: bit x % 32 of word x / 32 says that token x may come
+ *   workspace: loza_ssa_token_probs_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
+ * Token x with logit l, said c times: l / repetition if l > 0, l repetition otherwise, where it was said or occurs in the prompt; less frequency c and
+ * (c > 0) presence; plus its bias; each operation rounded to fp32. Tokens that are not allowed, whatever their logits, and those whose result is a NaN, weigh
+ * nothing. probs = exp((l - max) / temperature) / sum; where the temperature is not in [2^-126, 2^126] (0: greedy): 1 at the first of the largest. A row in
+ * which nothing weighs is all 0 (loza_ssa_verify_tree then has no next token). Logits of +infinity share a row among them.
+ * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30, as many rows as a launch takes. Sums in fp32, always in the same order.
+ */
+#define LOZA_MAX_BIAS 1024
+size_t loza_ssa_token_probs_workspace_bytes(int B, int n, int V);
+int loza_ssa_token_probs(const void *logits, int64_t logits_row, const int32_t *tree_lens, const int32_t *tokens, const int64_t *masks,
+                         const uint16_t *seen, int64_t seen_row, const float *repetition, const float *frequency, const float *presence,
+                         const float *temperature, const int32_t *bias_tokens, const float *bias_values, int n_bias, const int32_t *allowed,
+                         float *probs, int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream);
+int loza_ssa_token_probs_f32(const float *logits, int64_t logits_row, const int32_t *tree_lens, const int32_t *tokens, const int64_t *masks,
+                             const uint16_t *seen, int64_t seen_row, const float *repetition, const float *frequency, const float *presence,
+                             const float *temperature, const int32_t *bias_tokens, const float *bias_values, int n_bias, const int32_t *allowed,
+                             float *probs, int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The record that loza_ssa_token_probs reads, kept up to date: the first lens[b] entries of request b are taken note of, those before prompt_lens[b] as
+ * tokens of its prompt, the others as said once more (up to 32,767 times).
+ *   tokens [B, n] int32; path [B, n] int32 or NULL: entry i is tokens[b, path[b, i]] in the place of tokens[b, i] (entries outside [0, n) are skipped, and so are
+ *           tokens outside [0, V)); a step: the tokens of its trees, path and path_lens of loza_ssa_verify_tree
+ *   lens [B] int32 (cut to [0, n]), prompt_lens [B] int32 or NULL (none)
+ *   fresh [B] int32 or NULL: where it is not 0, the request's row is cleared first (a new request, with its prompt and what it has said already)
+ *   seen [B] rows, seen_row elements apart, as above
+ * B <= 65535, n <= 2^30, V <= 2^30. The result does not depend on the order of the entries.
+ */
+int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int32_t *lens, const int32_t *prompt_lens, const int32_t *fresh,
+                          uint16_t *seen, int64_t seen_row, int B, int n, int V, void *stream);
+
+/*
+ * Pages that several requests hold, and pages given back. shared [num_pages] int32 says how many requests beyond the first hold a page (0 for pages
+ * that are free or held by one; loza_ssa_step_tables deals out pages of 0). trimmed [B] int32 says which pages of a request have been given back while it goes
+ * on: entries [sink_pages, trimmed) of its row of block_table, sink_pages = ceil(sink_blocks block / page_size); 0: none. Those entries stay as they are and mean
+ * nothing: no query reads them any more. (A table that layers with another pattern, or without one, read as well, must not be trimmed.) NULL for both of
+ * trimmed and trimmed_after: no request is. All calls change none of their inputs but those named, so they can be repeated; results may not overlap other
+ * arrays of the call (LOZA_ERR_SHAPE). Numbers of requests out of range (lengths or held negative or beyond max_pages_per_seq pages): the request is left out.
+ *
+ * loza_ssa_pages_fork: request b becomes a copy of request from[b] (outside [0, B): no fork). Its place must be empty (cache_lens[b] and held[b] 0). It shares
+ * the source's full pages and gets a new one for a page that is started, into which loza_ssa_pages_copy brings the rows; so neither writes where the other reads
+ * as long as both only add rows. Several requests may have one source.
+ *   cache_lens, held [B], free_pages, free_count, block_table: as loza_ssa_step_tables_held; entries of the forks' rows of block_table are written. New pages are dealt
+ *           out as there, in the order of the requests; a fork that needs one when none is left is not made
+ *   forked [B] int32: 1 for each fork made, 0 otherwise     cache_lens_after, held_after, trimmed_after [B]: the forks' as their sources', the others' as given
+ *   copy_from, copy_to, copy_rows [B] int32: the started page, where its rows go, and how many; -1, -1, 0 where there is none
+ *   free_left [1]     shared_after [num_pages]: shared and the new holders
+ * loza_ssa_pages_copy: rows of page from[i] to page to[i] in each of n_layers caches k_pages [n_layers, num_pages, page_size, k_row_bytes], and v_pages likewise
+ * (NULL: none), the first rows[i] of them (NULL: all). count [1] int32 or NULL: entries of the lists that are valid, at most n. Entries with a page outside
+ * [0, num_pages) are skipped. A page that is written must not be read, or written by another entry. Row sizes: multiples of 16 bytes, up to 2^24; page_size <= 2^20.
+ *
+ * loza_ssa_pages_free: gives back what requests hold no longer: all pages of those that end (ending[b] not 0; ending NULL: none), and of the others (with
+ * trimmed) the pages behind the sink that no query at position cache_lens[b] or later sees under the pattern. A page goes to the free list when its last holder has given it up.
+ *   free_pages [num_free] (num_free >= num_pages): the freed pages are written behind the first free_count entries, in the order of their numbers
+ *   cache_lens_after, held_after, trimmed_after [B]: 0 for requests that end     free_after [1]: the new free_count     shared_after [num_pages]
+ *   shared and shared_after NULL: every page has one holder
+ *   workspace: loza_ssa_pages_free_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
+ *
+ * loza_ssa_pages_compact: with u pages in use (all that are not in the free list), those with numbers from u on become, in order, the free ones below u, so that the
+ * pool can be cut to u pages. Whoever names pages by number in other places has to be told. loza_ssa_pages_copy (count = n_copies) moves the rows.
+ *   table_after [B, max_pages_per_seq]: block_table with the new numbers (entries that are no pages in use as they are)
+ *   free_pages_after [num_free]: num_pages - 1 down to u, then -1     free_after [1]     shared_after [num_pages]: by the new numbers
+ *   copy_from, copy_to [num_pages / 2] int32: the moves, then -1     n_copies [1]     shared and shared_after, workspace: as above; num_pages >= 2
+ */
+int loza_ssa_pages_fork(const int32_t *from, const int32_t *cache_lens, const int32_t *held, const int32_t *trimmed, const int32_t *free_pages,
+                        const int32_t *free_count, const int32_t *shared, int32_t *block_table, int B, int64_t num_free, int64_t num_pages,
+                        int page_size, int max_pages_per_seq, int64_t sink_blocks, int64_t block, int32_t *forked, int32_t *cache_lens_after,
+                        int32_t *held_after, int32_t *trimmed_after, int32_t *copy_from, int32_t *copy_to, int32_t *copy_rows, int32_t *free_left,
+                        int32_t *shared_after, void *stream);
+int loza_ssa_pages_copy(void *k_pages, void *v_pages, const int32_t *from, const int32_t *to, const int32_t *rows, const int32_t *count, int64_t n,
+                        int n_layers, int64_t num_pages, int page_size, int64_t k_row_bytes, int64_t v_row_bytes, void *stream);
+size_t loza_ssa_pages_free_workspace_bytes(int64_t num_pages);
+int loza_ssa_pages_free(const int32_t *ending, const int32_t *cache_lens, const int32_t *held, const int32_t *trimmed, const int32_t *block_table,
+                        const int32_t *shared, int32_t *free_pages, const int32_t *free_count, int B, int64_t num_free, int64_t num_pages, int page_size,
+                        int max_pages_per_seq, int64_t sink_blocks, int64_t local_blocks, int64_t block, int32_t *cache_lens_after, int32_t *held_after,
+                        int32_t *trimmed_after, int32_t *free_after, int32_t *shared_after, void *workspace, size_t workspace_bytes, void *stream);
+size_t loza_ssa_pages_compact_workspace_bytes(int64_t num_pages);
+int loza_ssa_pages_compact(const int32_t *block_table, const int32_t *free_pages, const int32_t *free_count, const int32_t *shared, int B, int64_t num_free,
+                           int64_t num_pages, int max_pages_per_seq, int32_t *table_after, int32_t *free_pages_after, int32_t *free_after,
+                           int32_t *shared_after, int32_t *copy_from, int32_t *copy_to, int32_t *n_copies, void *workspace, size_t workspace_bytes,
+                           void *stream);
 
 /* Host-only (ours). Static string naming a status code. */
 const char *loza_status_str(int status);

@@ -24,4 +24,9 @@ from .binding import (  # noqa: F401
     loza_ssa_step_tables, loza_ssa_rope, loza_ssa_rope_f32, loza_ssa_rope_append, loza_ssa_rope_append_f32, loza_ssa_rope_frequencies,
     loza_ssa_extend_tree, loza_ssa_extend_tree_workspace_bytes, loza_ssa_extend_tree_kernel, loza_ssa_verify_tree, loza_ssa_verify_tree_workspace_bytes,
     loza_ssa_keep_accepted, LOZA_TREE_MAX_NODES,
+    loza_ssa_norm_rope, loza_ssa_norm_rope_f32, loza_ssa_norm_rope_backward, loza_ssa_norm_rope_backward_f32,
+    loza_ssa_norm_rope_backward_workspace_bytes, loza_ssa_norm_rope_append, loza_ssa_norm_rope_append_f32,
+    loza_ssa_token_probs, loza_ssa_token_probs_f32, loza_ssa_token_probs_workspace_bytes, loza_ssa_count_tokens,
+    loza_ssa_pages_fork, loza_ssa_pages_copy, loza_ssa_pages_free, loza_ssa_pages_free_workspace_bytes,
+    loza_ssa_pages_compact, loza_ssa_pages_compact_workspace_bytes,
 )

@@ -43,6 +43,11 @@ EXPORTS = (
     "loza_ssa_rope_frequencies", "loza_ssa_extend_tree", "loza_ssa_extend_tree_workspace_bytes",
     "loza_ssa_extend_tree_kernel",
     "loza_ssa_verify_tree", "loza_ssa_verify_tree_workspace_bytes", "loza_ssa_keep_accepted",
+    "loza_ssa_norm_rope", "loza_ssa_norm_rope_f32", "loza_ssa_norm_rope_backward_workspace_bytes", "loza_ssa_norm_rope_backward",
+    "loza_ssa_norm_rope_backward_f32", "loza_ssa_norm_rope_append", "loza_ssa_norm_rope_append_f32",
+    "loza_ssa_token_probs_workspace_bytes", "loza_ssa_token_probs", "loza_ssa_token_probs_f32", "loza_ssa_count_tokens",
+    "loza_ssa_pages_fork", "loza_ssa_pages_copy", "loza_ssa_pages_free_workspace_bytes", "loza_ssa_pages_free",
+    "loza_ssa_pages_compact_workspace_bytes", "loza_ssa_pages_compact",
 )
 KERNEL_TILES, KERNEL_ROWS, KERNEL_D128 = 1, 2, 3
 
@@ -160,6 +165,36 @@ def lib() -> ctypes.CDLL:
         L.loza_ssa_verify_tree_workspace_bytes.argtypes = [ci, ci, ci]
         L.loza_ssa_keep_accepted.restype = ci
         L.loza_ssa_keep_accepted.argtypes = [vp] * 5 + [ci, ci, ci, i64, i64, i64, vp]
+        for name in ("loza_ssa_norm_rope", "loza_ssa_norm_rope_f32"):
+            getattr(L, name).restype = ci
+            getattr(L, name).argtypes = [vp] * 5 + [i64, ci, ci] + [i64] * 4 + [ci, ci, f32, ci, ci, ci, f32, vp]
+        L.loza_ssa_norm_rope_backward_workspace_bytes.restype = sz
+        L.loza_ssa_norm_rope_backward_workspace_bytes.argtypes = [i64, ci, ci, ci]
+        for name in ("loza_ssa_norm_rope_backward", "loza_ssa_norm_rope_backward_f32"):
+            getattr(L, name).restype = ci
+            getattr(L, name).argtypes = [vp] * 7 + [i64, ci, ci] + [i64] * 6 + [ci, ci, f32, ci, ci, ci, f32, vp, sz, vp]
+        for name in ("loza_ssa_norm_rope_append", "loza_ssa_norm_rope_append_f32"):
+            getattr(L, name).restype = ci
+            getattr(L, name).argtypes = [vp] * 11 + [i64] + [ci] * 5 + [i64] * 9 + [ci] * 4 + [f32] + [ci] * 4 + [f32, vp]
+        L.loza_ssa_token_probs_workspace_bytes.restype = sz
+        L.loza_ssa_token_probs_workspace_bytes.argtypes = [ci, ci, ci]
+        for name in ("loza_ssa_token_probs", "loza_ssa_token_probs_f32"):
+            getattr(L, name).restype = ci
+            getattr(L, name).argtypes = [vp, i64, vp, vp, vp, vp, i64] + [vp] * 6 + [ci, vp, vp, ci, ci, ci, vp, sz, vp]
+        L.loza_ssa_count_tokens.restype = ci
+        L.loza_ssa_count_tokens.argtypes = [vp] * 6 + [i64, ci, ci, ci, vp]
+        L.loza_ssa_pages_fork.restype = ci
+        L.loza_ssa_pages_fork.argtypes = [vp] * 8 + [ci, i64, i64, ci, ci, i64, i64] + [vp] * 10
+        L.loza_ssa_pages_copy.restype = ci
+        L.loza_ssa_pages_copy.argtypes = [vp] * 6 + [i64, ci, i64, ci, i64, i64, vp]
+        L.loza_ssa_pages_free_workspace_bytes.restype = sz
+        L.loza_ssa_pages_free_workspace_bytes.argtypes = [i64]
+        L.loza_ssa_pages_free.restype = ci
+        L.loza_ssa_pages_free.argtypes = [vp] * 8 + [ci, i64, i64, ci, ci, i64, i64, i64] + [vp] * 6 + [sz, vp]
+        L.loza_ssa_pages_compact_workspace_bytes.restype = sz
+        L.loza_ssa_pages_compact_workspace_bytes.argtypes = [i64]
+        L.loza_ssa_pages_compact.restype = ci
+        L.loza_ssa_pages_compact.argtypes = [vp] * 4 + [ci, i64, i64, ci] + [vp] * 8 + [sz, vp]
         # (of the HIP runtime that the library is linked with)
         L.hipThreadExchangeStreamCaptureMode.restype = ci
         L.hipThreadExchangeStreamCaptureMode.argtypes = [ctypes.POINTER(ci)]
@@ -883,3 +918,247 @@ def loza_ssa_keep_accepted(k_rows, v_rows, slots, path, path_lens, stream=None):
     _call("loza_ssa_keep_accepted", _ptr(k_rows, k_rows.dtype, None, "k_rows", dev), None if v_rows is None else _ptr(v_rows, v_rows.dtype, None, "v_rows", dev),
           _ptr(slots, i32, None, "slots", dev), _ptr(path, i32, (B, n), "path", dev), _ptr(path_lens, i32, (B,), "path_lens", dev), B, n, layers,
           math.prod(lead), hk * dk * k_rows.element_size(), v_bytes, _stream(stream))
+
+
+# ---- norms with rotary positions ----
+
+def _norm_rope(fn_name, dtype, x, weight, positions, freq, out, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale, stream):
+    dev, shape, (pairs,) = _launch_device(x), x.shape, freq.shape
+    T, H, d = shape
+    xp, xt, xh = _heads(x, dtype, shape, "x", dev)
+    op, ot, oh = _heads(out, dtype, shape, "out", dev)
+    _call(fn_name, xp, _ptr(weight, torch.float32, (norm_dim,), "weight", dev), _ptr(positions, torch.int32, (T,), "positions", dev),
+          _ptr(freq, torch.float64, None, "freq", dev), op, T, H, d, xt, xh, ot, oh, int(norm_begin), int(norm_dim), float(eps), int(rot_begin), 2 * pairs,
+          bool(interleaved), float(mscale), _stream(stream))
+
+
+def loza_ssa_norm_rope(x, weight, positions, freq, out, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale=1.0, stream=None):
+    """Norm of each head (columns [norm_begin, norm_begin + norm_dim), weight [norm_dim] float32 or None) and rotary positions (columns
+    [rot_begin, rot_begin + 2 len(freq))) of x [T,H,d] bf16 into out, in one pass. Strides, positions, freq, in place: as :func:`loza_ssa_rope`."""
+    _norm_rope("loza_ssa_norm_rope", torch.bfloat16, x, weight, positions, freq, out, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale, stream)
+
+
+def loza_ssa_norm_rope_f32(x, weight, positions, freq, out, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale=1.0, stream=None):
+    """fp32 twin of :func:`loza_ssa_norm_rope`."""
+    _norm_rope("loza_ssa_norm_rope_f32", torch.float32, x, weight, positions, freq, out, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale, stream)
+
+
+def loza_ssa_norm_rope_backward_workspace_bytes(T, H, d, norm_dim) -> int:
+    return int(lib().loza_ssa_norm_rope_backward_workspace_bytes(int(T), int(H), int(d), int(norm_dim)))
+
+
+def _norm_rope_backward(fn_name, dtype, dout, x, weight, positions, freq, dx, dweight, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale, workspace, stream):
+    dev, shape, (pairs,) = _launch_device(x), x.shape, freq.shape
+    T, H, d = shape
+    gp, gt, gh = _heads(dout, dtype, shape, "dout", dev)
+    xp, xt, xh = _heads(x, dtype, shape, "x", dev)
+    op, ot, oh = _heads(dx, dtype, shape, "dx", dev)
+    f32 = torch.float32
+    if dweight is not None and workspace is None:
+        workspace = _scratch(loza_ssa_norm_rope_backward_workspace_bytes(T, H, d, norm_dim), stream)
+    _call(fn_name, gp, xp, _ptr(weight, f32, (norm_dim,), "weight", dev), _ptr(positions, torch.int32, (T,), "positions", dev),
+          _ptr(freq, torch.float64, None, "freq", dev), op, _ptr(dweight, f32, (norm_dim,), "dweight", dev), T, H, d, gt, gh, xt, xh, ot, oh, int(norm_begin),
+          int(norm_dim), float(eps), int(rot_begin), 2 * pairs, bool(interleaved), float(mscale), _ptr(workspace, torch.uint8, None, "workspace", dev),
+          0 if workspace is None else workspace.numel(), _stream(stream))
+
+
+def loza_ssa_norm_rope_backward(dout, x, weight, positions, freq, dx, dweight, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale=1.0, workspace=None,
+                                stream=None):
+    """Gradient of :func:`loza_ssa_norm_rope`: dx [T,H,d] bf16 (may be dout or x) and dweight [norm_dim] float32 (None: not wanted) from dout and the forward's
+    x. workspace: uint8, ``loza_ssa_norm_rope_backward_workspace_bytes``; None: from torch's allocator (while a stream is captured there is none to
+    be had, and a call that needs one is refused)."""
+    _norm_rope_backward("loza_ssa_norm_rope_backward", torch.bfloat16, dout, x, weight, positions, freq, dx, dweight, norm_begin, norm_dim, eps, rot_begin,
+                        interleaved, mscale, workspace, stream)
+
+
+def loza_ssa_norm_rope_backward_f32(dout, x, weight, positions, freq, dx, dweight, norm_begin, norm_dim, eps, rot_begin, interleaved, mscale=1.0, workspace=None,
+                                    stream=None):
+    """fp32 twin of :func:`loza_ssa_norm_rope_backward`."""
+    _norm_rope_backward("loza_ssa_norm_rope_backward_f32", torch.float32, dout, x, weight, positions, freq, dx, dweight, norm_begin, norm_dim, eps, rot_begin,
+                        interleaved, mscale, workspace, stream)
+
+
+def _norm_rope_append(fn_name, dtype, q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, q_norm_begin, q_norm_dim, k_norm_begin,
+                      k_norm_dim, eps, q_rot_begin, k_rot_begin, interleaved, mscale, stream):
+    dev, i32, f32, (pairs,) = _launch_device(k), torch.int32, torch.float32, freq.shape
+    T, Hkv, d_k = k.shape
+    *lead, hk, dk = k_rows.shape
+    if not lead or (hk, dk) != (Hkv, d_k):
+        raise ValueError("k_rows must be [..., Hkv, d_k]")
+    if (q is None) != (q_out is None) or (v is None) != (v_rows is None):
+        raise ValueError("q and q_out go together, and so do v and v_rows")
+    rows, Hq, d_q, d_v = math.prod(lead), 0, 0, 0
+    if q is not None:
+        _, Hq, d_q = q.shape
+    if v is not None:
+        d_v = v.shape[-1]
+    qp, qt, qh = _heads(q, dtype, (T, Hq, d_q), "q", dev)
+    op, ot, oh = _heads(q_out, dtype, (T, Hq, d_q), "q_out", dev)
+    kp, kt, kh = _heads(k, dtype, (T, Hkv, d_k), "k", dev)
+    vp, vt, vh = _heads(v, dtype, (T, Hkv, d_v), "v", dev)
+    _call(fn_name, qp, _ptr(q_weight, f32, (q_norm_dim,), "q_weight", dev), kp, _ptr(k_weight, f32, (k_norm_dim,), "k_weight", dev), vp,
+          _ptr(positions, i32, (T,), "positions", dev), _ptr(slots, i32, (T,), "slots", dev), _ptr(freq, torch.float64, None, "freq", dev), op,
+          _ptr(k_rows, dtype, None, "k_rows", dev), _ptr(v_rows, dtype, (*lead, Hkv, d_v), "v_rows", dev), T, Hq, Hkv, d_q, d_k, d_v, qt, qh, ot, oh, kt, kh, vt, vh,
+          rows, int(q_norm_begin), int(q_norm_dim), int(k_norm_begin), int(k_norm_dim), float(eps), int(q_rot_begin), int(k_rot_begin), 2 * pairs,
+          bool(interleaved), float(mscale), _stream(stream))
+
+
+def loza_ssa_norm_rope_append(q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, q_norm_begin, q_norm_dim, k_norm_begin, k_norm_dim,
+                              eps, q_rot_begin, k_rot_begin, interleaved, mscale=1.0, stream=None):
+    """:func:`loza_ssa_rope_append` with the norms of :func:`loza_ssa_norm_rope`: q and k are normed (q_weight [q_norm_dim], k_weight [k_norm_dim] float32 or
+    None: ones; a norm_dim of 0: not normed) and rotated, k and v go to row slots[t] of the cache."""
+    _norm_rope_append("loza_ssa_norm_rope_append", torch.bfloat16, q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, q_norm_begin,
+                      q_norm_dim, k_norm_begin, k_norm_dim, eps, q_rot_begin, k_rot_begin, interleaved, mscale, stream)
+
+
+def loza_ssa_norm_rope_append_f32(q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, q_norm_begin, q_norm_dim, k_norm_begin, k_norm_dim,
+                                  eps, q_rot_begin, k_rot_begin, interleaved, mscale=1.0, stream=None):
+    """fp32 twin of :func:`loza_ssa_norm_rope_append`."""
+    _norm_rope_append("loza_ssa_norm_rope_append_f32", torch.float32, q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, q_norm_begin,
+                      q_norm_dim, k_norm_begin, k_norm_dim, eps, q_rot_begin, k_rot_begin, interleaved, mscale, stream)
+
+
+# ---- probabilities from logits ----
+
+def loza_ssa_token_probs_workspace_bytes(B, n, V) -> int:
+    return int(lib().loza_ssa_token_probs_workspace_bytes(int(B), int(n), int(V)))
+
+
+def _seen(seen, B, dev):
+    """(pointer, row stride) of a record [B, row] int16 on that device."""
+    return (None, 0) if seen is None else (_ptr(seen, torch.int16, (B, seen.shape[-1]), "seen", dev), seen.shape[-1])
+
+
+def _token_probs(fn_name, dtype, logits, probs, workspace, tree_lens, tokens, masks, seen, repetition, frequency, presence, temperature, bias_tokens, bias_values,
+                 allowed, stream):
+    dev, f32, i32 = _launch_device(logits), torch.float32, torch.int32
+    B, n, V = logits.shape
+    rows, both = (B,), (B, n)
+    sb, sn, sv = logits.stride()
+    row = sn if n > 1 else sb if B > 1 else V
+    if logits.dtype is not dtype or (sv != 1 and V > 1) or (B > 1 and sb != n * row) or logits.get_device() != dev:
+        _dev_ptr(logits.contiguous(), dtype, "logits")
+        raise ValueError("the rows of logits must lie one behind the other, at any distance, on the current device")
+    if (tokens is None) != (masks is None) or (bias_tokens is None) != (bias_values is None):
+        raise ValueError("tokens and masks go together, and so do bias_tokens and bias_values")
+    n_bias = 0 if bias_tokens is None else bias_tokens.shape[-1]
+    sp, seen_row = _seen(seen, B, dev)
+    if workspace is None:
+        workspace = _scratch(loza_ssa_token_probs_workspace_bytes(B, n, V), stream)
+    _call(fn_name, logits.data_ptr(), row, _ptr(tree_lens, i32, rows, "tree_lens", dev), _ptr(tokens, i32, both, "tokens", dev),
+          _ptr(masks, torch.int64, both, "masks", dev), sp, seen_row, _ptr(repetition, f32, rows, "repetition", dev), _ptr(frequency, f32, rows, "frequency", dev),
+          _ptr(presence, f32, rows, "presence", dev), _ptr(temperature, f32, rows, "temperature", dev), _ptr(bias_tokens, i32, (B, n_bias), "bias_tokens", dev),
+          _ptr(bias_values, f32, (B, n_bias), "bias_values", dev), n_bias, _ptr(allowed, i32, (B, n, (V + 31) // 32), "allowed", dev),
+          _ptr(probs, f32, (B, n, V), "probs", dev), B, n, V, _ptr(workspace, torch.uint8, None, "workspace", dev), 0 if workspace is None else workspace.numel(),
+          _stream(stream))
+
+
+def loza_ssa_token_probs(logits, probs, workspace=None, tree_lens=None, tokens=None, masks=None, seen=None, repetition=None, frequency=None, presence=None,
+                         temperature=None, bias_tokens=None, bias_values=None, allowed=None, stream=None):
+    """Probabilities (probs [B,n,V] float32) from logits [B,n,V] bf16 (rows at any distance from each other) under penalties, biases, grammar masks and
+    temperatures. tree_lens [B], tokens [B,n] int32, masks [B,n] int64: the trees; seen [B,row] int16: :func:`loza_ssa_count_tokens`; repetition, frequency,
+    presence, temperature [B] float32; bias_tokens [B,m] int32 and bias_values [B,m] float32; allowed [B,n,ceil(V/32)] int32. workspace: uint8,
+    ``loza_ssa_token_probs_workspace_bytes``; None: from torch's allocator (while a stream is captured: refused)."""
+    _token_probs("loza_ssa_token_probs", torch.bfloat16, logits, probs, workspace, tree_lens, tokens, masks, seen, repetition, frequency, presence, temperature,
+                 bias_tokens, bias_values, allowed, stream)
+
+
+def loza_ssa_token_probs_f32(logits, probs, workspace=None, tree_lens=None, tokens=None, masks=None, seen=None, repetition=None, frequency=None, presence=None,
+                             temperature=None, bias_tokens=None, bias_values=None, allowed=None, stream=None):
+    """fp32 twin of :func:`loza_ssa_token_probs`; ``probs`` may be the (contiguous) logits themselves."""
+    _token_probs("loza_ssa_token_probs_f32", torch.float32, logits, probs, workspace, tree_lens, tokens, masks, seen, repetition, frequency, presence, temperature,
+                 bias_tokens, bias_values, allowed, stream)
+
+
+def loza_ssa_count_tokens(tokens, lens, seen, V, path=None, prompt_lens=None, fresh=None, stream=None):
+    """Takes note of the first lens[b] of tokens [B,n] int32 (``path`` [B,n]: of tokens[b, path[b, i]]) in seen [B,row] int16 (row a multiple of 8, >= V): those
+    before prompt_lens[b] as tokens of the prompt, the others as said once more. fresh [B]: rows that are cleared first where it is not 0."""
+    dev, i32 = _launch_device(tokens), torch.int32
+    B, n = tokens.shape
+    sp, seen_row = _seen(seen, B, dev)
+    _call("loza_ssa_count_tokens", _ptr(tokens, i32, None, "tokens", dev), _ptr(path, i32, (B, n), "path", dev), _ptr(lens, i32, (B,), "lens", dev),
+          _ptr(prompt_lens, i32, (B,), "prompt_lens", dev), _ptr(fresh, i32, (B,), "fresh", dev), sp, seen_row, B, n, int(V), _stream(stream))
+
+
+# ---- pages ----
+
+def loza_ssa_pages_fork(from_, cache_lens, held, trimmed, free_pages, free_count, shared, block_table, num_pages, page_size, sink_blocks, block, forked,
+                        cache_lens_after, held_after, trimmed_after, copy_from, copy_to, copy_rows, free_left, shared_after, stream=None):
+    """Request b becomes a copy of request from_[b] (-1: no fork) that shares its full pages. All int32 on the GPU: from_, cache_lens, held, forked, copy_from,
+    copy_to, copy_rows, the ``_after`` of the first three [B], trimmed and trimmed_after [B] (or both None), free_pages [F], free_count and free_left [1], shared and
+    shared_after [num_pages], block_table [B,max_pages], whose rows of the forks are written."""
+    dev, i32 = _launch_device(from_), torch.int32
+    (B,), (num_free,), most = from_.shape, free_pages.shape, block_table.shape[-1]
+    rows, pages = (B,), (int(num_pages),)
+    if (trimmed is None) != (trimmed_after is None):
+        raise ValueError("trimmed and trimmed_after must both be [B], or both None")
+    _call("loza_ssa_pages_fork", _ptr(from_, i32, rows, "from_", dev), _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(held, i32, rows, "held", dev),
+          _ptr(trimmed, i32, rows, "trimmed", dev), _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev),
+          _ptr(shared, i32, pages, "shared", dev), _ptr(block_table, i32, (B, most), "block_table", dev), B, num_free, int(num_pages), int(page_size), most,
+          int(sink_blocks), int(block), _ptr(forked, i32, rows, "forked", dev), _ptr(cache_lens_after, i32, rows, "cache_lens_after", dev),
+          _ptr(held_after, i32, rows, "held_after", dev), _ptr(trimmed_after, i32, rows, "trimmed_after", dev), _ptr(copy_from, i32, rows, "copy_from", dev),
+          _ptr(copy_to, i32, rows, "copy_to", dev), _ptr(copy_rows, i32, rows, "copy_rows", dev), _ptr(free_left, i32, (1,), "free_left", dev),
+          _ptr(shared_after, i32, pages, "shared_after", dev), _stream(stream))
+
+
+def loza_ssa_pages_copy(k_pages, v_pages, from_, to, rows=None, count=None, stream=None):
+    """Page from_[i] to page to[i] of k_pages [layers,num_pages,page_size,Hkv,d] (any type) and v_pages likewise (or None), the first rows[i] rows of it (None:
+    all). from_, to, rows [n], count [1] (None: n) int32; entries that are no pages are skipped."""
+    dev, i32 = _launch_device(k_pages), torch.int32
+    layers, pages, size, hk, dk = k_pages.shape
+    (n,) = from_.shape
+    if v_pages is not None and v_pages.shape[:3] != k_pages.shape[:3]:
+        raise ValueError("v_pages must be of the same layers and pages as k_pages")
+    v_bytes = 0 if v_pages is None else v_pages.shape[-2] * v_pages.shape[-1] * v_pages.element_size()
+    _call("loza_ssa_pages_copy", _ptr(k_pages, k_pages.dtype, None, "k_pages", dev), None if v_pages is None else _ptr(v_pages, v_pages.dtype, None, "v_pages", dev),
+          _ptr(from_, i32, None, "from_", dev), _ptr(to, i32, (n,), "to", dev), _ptr(rows, i32, (n,), "rows", dev), _ptr(count, i32, (1,), "count", dev), n, layers,
+          pages, size, hk * dk * k_pages.element_size(), v_bytes, _stream(stream))
+
+
+def loza_ssa_pages_free_workspace_bytes(num_pages) -> int:
+    return int(lib().loza_ssa_pages_free_workspace_bytes(int(num_pages)))
+
+
+def loza_ssa_pages_free(ending, cache_lens, held, trimmed, block_table, shared, free_pages, free_count, num_pages, page_size, sink_blocks, local_blocks, block,
+                        cache_lens_after, held_after, trimmed_after, free_after, shared_after, workspace=None, stream=None):
+    """Gives back the pages of the requests that end (ending [B] not 0; None: none do) and, with trimmed, those that no later query of the others sees. All int32 on
+    the GPU: cache_lens, held and their ``_after`` [B], trimmed and trimmed_after [B] (or both None), block_table [B,max_pages], shared and shared_after [num_pages]
+    (or both None), free_pages [F >= num_pages], written behind its first free_count [1] entries, free_after [1]. workspace: uint8,
+    ``loza_ssa_pages_free_workspace_bytes``; None: from torch's allocator (while a stream is captured: refused)."""
+    dev, i32 = _launch_device(cache_lens), torch.int32
+    (B,), (num_free,), most = cache_lens.shape, free_pages.shape, block_table.shape[-1]
+    rows, pages = (B,), (int(num_pages),)
+    if (trimmed is None) != (trimmed_after is None) or (shared is None) != (shared_after is None):
+        raise ValueError("trimmed and trimmed_after go together, and so do shared and shared_after")
+    if workspace is None:
+        workspace = _scratch(loza_ssa_pages_free_workspace_bytes(num_pages), stream)
+    _call("loza_ssa_pages_free", _ptr(ending, i32, rows, "ending", dev), _ptr(cache_lens, i32, rows, "cache_lens", dev), _ptr(held, i32, rows, "held", dev),
+          _ptr(trimmed, i32, rows, "trimmed", dev), _ptr(block_table, i32, (B, most), "block_table", dev), _ptr(shared, i32, pages, "shared", dev),
+          _ptr(free_pages, i32, None, "free_pages", dev), _ptr(free_count, i32, (1,), "free_count", dev), B, num_free, int(num_pages), int(page_size), most,
+          int(sink_blocks), _win(local_blocks), int(block), _ptr(cache_lens_after, i32, rows, "cache_lens_after", dev),
+          _ptr(held_after, i32, rows, "held_after", dev), _ptr(trimmed_after, i32, rows, "trimmed_after", dev), _ptr(free_after, i32, (1,), "free_after", dev),
+          _ptr(shared_after, i32, pages, "shared_after", dev), _ptr(workspace, torch.uint8, None, "workspace", dev), 0 if workspace is None else workspace.numel(),
+          _stream(stream))
+
+
+def loza_ssa_pages_compact_workspace_bytes(num_pages) -> int:
+    return int(lib().loza_ssa_pages_compact_workspace_bytes(int(num_pages)))
+
+
+def loza_ssa_pages_compact(block_table, free_pages, free_count, shared, num_pages, table_after, free_pages_after, free_after, shared_after, copy_from, copy_to,
+                           n_copies, workspace=None, stream=None):
+    """New numbers for the pages of a pool, those in use first, and the copies that this takes (:func:`loza_ssa_pages_copy` with ``count=n_copies``). All int32 on the
+    GPU: block_table and table_after [B,max_pages], free_pages and free_pages_after [F >= num_pages], free_count, free_after, n_copies [1], shared and shared_after
+    [num_pages] (or both None), copy_from and copy_to [num_pages // 2]. workspace: uint8, ``loza_ssa_pages_compact_workspace_bytes``, as for the others."""
+    dev, i32 = _launch_device(block_table), torch.int32
+    (B, most), (num_free,), pages, half = block_table.shape, free_pages.shape, (int(num_pages),), (int(num_pages) // 2,)
+    if (shared is None) != (shared_after is None):
+        raise ValueError("shared and shared_after must both be [num_pages], or both None")
+    if workspace is None:
+        workspace = _scratch(loza_ssa_pages_compact_workspace_bytes(num_pages), stream)
+    _call("loza_ssa_pages_compact", _ptr(block_table, i32, None, "block_table", dev), _ptr(free_pages, i32, None, "free_pages", dev),
+          _ptr(free_count, i32, (1,), "free_count", dev), _ptr(shared, i32, pages, "shared", dev), B, num_free, int(num_pages), most,
+          _ptr(table_after, i32, (B, most), "table_after", dev), _ptr(free_pages_after, i32, (num_free,), "free_pages_after", dev),
+          _ptr(free_after, i32, (1,), "free_after", dev), _ptr(shared_after, i32, pages, "shared_after", dev), _ptr(copy_from, i32, half, "copy_from", dev),
+          _ptr(copy_to, i32, half, "copy_to", dev), _ptr(n_copies, i32, (1,), "n_copies", dev), _ptr(workspace, torch.uint8, None, "workspace", dev),
+          0 if workspace is None else workspace.numel(), _stream(stream))

@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <stdlib.h>
 
+#include <initializer_list>
 #include <mutex>
 
 #include "../../include/loza_ssa.h"
@@ -1234,6 +1235,21 @@ int loza_ssa_extend_tree_kernel(int B, int Hq, int Hkv, int64_t S_max, int n, in
     return plan.kernel;
 }
 
+// Whether one of the first n_results arrays lies on another of the n arrays (null: not there)
+struct Span {
+    const void *ptr;
+    int64_t bytes;
+};
+static bool overlap(const Span *a, int n_results, int n)
+{
+    for (int i = 0; i < n_results; ++i)
+        for (int j = i + 1; j < n; ++j) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(a[i].ptr), y = reinterpret_cast<uintptr_t>(a[j].ptr);
+            if (x && y && (x <= y ? y - x < (uintptr_t)a[i].bytes : x - y < (uintptr_t)a[j].bytes)) return true;
+        }
+    return false;
+}
+
 static int step_tables(const int32_t *cache_lens, const int32_t *new_lens, const int32_t *parents, const int32_t *free_pages,
                        const int32_t *free_count, int32_t *block_table, int B, int n, int64_t num_free, int64_t num_pages,
                        int page_size, int max_pages_per_seq, int32_t *granted, int32_t *seqlens, int32_t *positions,
@@ -1256,15 +1272,10 @@ static int step_tables(const int32_t *cache_lens, const int32_t *new_lens, const
     if (reinterpret_cast<uintptr_t>(masks) & 7u) return LOZA_ERR_ALIGN;
     // a workgroup reads what another's results would be written over: no result may lie on anything else
     const int64_t b4 = 4LL * B, bn4 = b4 * n;
-    const struct { const void *ptr; int64_t bytes; } arrays[] = {
+    const Span arrays[] = {
         {granted, b4}, {seqlens, b4}, {positions, bn4}, {slots, bn4}, {masks, 2 * bn4}, {free_left, 4}, {held_after, b4}, {block_table, b4 * max_pages_per_seq},
         {cache_lens, b4}, {new_lens, b4}, {parents, bn4}, {free_pages, 4 * num_free}, {free_count, 4}, {held, b4}};
-    constexpr int n_results = 8, n_arrays = 14;
-    for (int i = 0; i < n_results; ++i)
-        for (int j = i + 1; j < n_arrays; ++j) {
-            const uintptr_t x = reinterpret_cast<uintptr_t>(arrays[i].ptr), y = reinterpret_cast<uintptr_t>(arrays[j].ptr);
-            if (x && y && (x <= y ? y - x < (uintptr_t)arrays[i].bytes : x - y < (uintptr_t)arrays[j].bytes)) return LOZA_ERR_SHAPE;
-        }
+    if (overlap(arrays, 8, 14)) return LOZA_ERR_SHAPE;
     loza::TablesParams p{};
     p.cache_lens = cache_lens; p.new_lens = new_lens; p.parents = parents; p.free_pages = free_pages; p.free_count = free_count;
     p.block_table = block_table; p.granted = granted; p.seqlens = seqlens; p.positions = positions; p.slots = slots;
@@ -1461,6 +1472,347 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     loza::KeepParams p{(char *)k_rows, (char *)v_rows, slots, path, path_lens, B, n, n_layers, cache_rows, k_row_bytes, v_rows ? v_row_bytes : 0};
     return loza::launch_keep_accepted(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+// ---- norms with rotary positions ------------------------------------------------------------------------
+
+// Checks what all calls of a norm with rotary positions share, and one of their tensors.
+static int check_norm_call(const loza::NormParams &p, bool normed)
+{
+    loza::RopeParams r{};
+    r.positions = p.positions; r.freq = p.freq; r.T = p.T; r.rot = p.rot; r.mscale = p.mscale;
+    if (int rc = check_rope(r)) return rc;
+    if (normed && !(p.eps >= 0x1p-126f && !isinf(p.eps))) return LOZA_ERR_SHAPE;
+    return LOZA_OK;
+}
+
+static int check_norm_heads(const loza::NormHeads &n, int64_t T, int rot, int es, bool out_strided)
+{
+    if (int rc = check_heads(n.r, T, rot, es, out_strided)) return rc;
+    if (n.r.d > LOZA_NORM_MAX_DIM || n.norm_begin < 0 || n.norm_dim < 0 || (int64_t)n.norm_begin + n.norm_dim > n.r.d) return LOZA_ERR_SHAPE;
+    return (reinterpret_cast<uintptr_t>(n.w) & 3u) ? LOZA_ERR_ALIGN : LOZA_OK;
+}
+
+static int norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                     int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
+                     int rot_begin, int rot_dim, int interleaved, float mscale, int es, void *stream)
+{
+    loza::NormParams p{};
+    p.q = {{x, out, x_token, x_head, out_token, out_head, H, d, rot_begin}, weight, norm_begin, norm_dim, 0};
+    p.positions = positions; p.freq = freq; p.T = T; p.rot = rot_dim; p.interleaved = interleaved != 0; p.mscale = mscale; p.eps = eps;
+    if (int rc = check_norm_call(p, true)) return rc;
+    if (int rc = check_norm_heads(p.q, T, rot_dim, es, true)) return rc;
+    if (norm_dim < 1) return LOZA_ERR_SHAPE;
+    return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
+                       int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
+                       int rot_begin, int rot_dim, int interleaved, float mscale, void *stream)
+{
+    return norm_rope(x, weight, positions, freq, out, T, H, d, x_token, x_head, out_token, out_head, norm_begin, norm_dim, eps, rot_begin, rot_dim,
+                     interleaved, mscale, 2, stream);
+}
+
+int loza_ssa_norm_rope_f32(const float *x, const float *weight, const int32_t *positions, const double *freq, float *out, int64_t T, int H, int d,
+                           int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
+                           int rot_begin, int rot_dim, int interleaved, float mscale, void *stream)
+{
+    return norm_rope(x, weight, positions, freq, out, T, H, d, x_token, x_head, out_token, out_head, norm_begin, norm_dim, eps, rot_begin, rot_dim,
+                     interleaved, mscale, 4, stream);
+}
+
+size_t loza_ssa_norm_rope_backward_workspace_bytes(int64_t T, int H, int d, int norm_dim)
+{
+    if (T < 1 || T > 2147483647LL || H < 1 || d < 1 || d > LOZA_NORM_MAX_DIM || (int64_t)H * d > 1 << 30 || norm_dim < 1 || norm_dim > d) return 0;
+    return (size_t)(T < loza::kNormPartials ? T : loza::kNormPartials) * norm_dim * sizeof(float);
+}
+
+static int norm_rope_backward(const void *dout, const void *x, const float *weight, const int32_t *positions, const double *freq, void *dx,
+                              float *dweight, int64_t T, int H, int d, int64_t dout_token, int64_t dout_head, int64_t x_token, int64_t x_head,
+                              int64_t dx_token, int64_t dx_head, int norm_begin, int norm_dim, float eps, int rot_begin, int rot_dim, int interleaved,
+                              float mscale, void *workspace, size_t workspace_bytes, int es, void *stream)
+{
+    loza::NormParams p{};
+    p.q = {{x, dx, x_token, x_head, dx_token, dx_head, H, d, rot_begin}, weight, norm_begin, norm_dim, 0};
+    p.positions = positions; p.freq = freq; p.T = T; p.rot = rot_dim; p.interleaved = interleaved != 0; p.mscale = mscale; p.eps = eps;
+    p.dout = dout; p.dout_token = dout_token; p.dout_head = dout_head; p.dw = dweight;
+    if (!dout) return LOZA_ERR_NULL;
+    if (int rc = check_norm_call(p, true)) return rc;
+    if (int rc = check_norm_heads(p.q, T, rot_dim, es, true)) return rc;
+    if (norm_dim < 1) return LOZA_ERR_SHAPE;
+    const loza::RopeHeads g{dout, dx, dout_token, dout_head, dx_token, dx_head, H, d, rot_begin};
+    if (int rc = check_heads(g, T, rot_dim, es, true)) return rc;
+    if (reinterpret_cast<uintptr_t>(dweight) & 3u) return LOZA_ERR_ALIGN;
+    if (dweight) {
+        if (!workspace || workspace_bytes < loza_ssa_norm_rope_backward_workspace_bytes(T, H, d, norm_dim)) return LOZA_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
+        p.partial = (float *)workspace;
+    }
+    return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_norm_rope_backward(const void *dout, const void *x, const float *weight, const int32_t *positions, const double *freq, void *dx,
+                                float *dweight, int64_t T, int H, int d, int64_t dout_token, int64_t dout_head, int64_t x_token, int64_t x_head,
+                                int64_t dx_token, int64_t dx_head, int norm_begin, int norm_dim, float eps, int rot_begin, int rot_dim,
+                                int interleaved, float mscale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return norm_rope_backward(dout, x, weight, positions, freq, dx, dweight, T, H, d, dout_token, dout_head, x_token, x_head, dx_token, dx_head,
+                              norm_begin, norm_dim, eps, rot_begin, rot_dim, interleaved, mscale, workspace, workspace_bytes, 2, stream);
+}
+
+int loza_ssa_norm_rope_backward_f32(const float *dout, const float *x, const float *weight, const int32_t *positions, const double *freq, float *dx,
+                                    float *dweight, int64_t T, int H, int d, int64_t dout_token, int64_t dout_head, int64_t x_token, int64_t x_head,
+                                    int64_t dx_token, int64_t dx_head, int norm_begin, int norm_dim, float eps, int rot_begin, int rot_dim,
+                                    int interleaved, float mscale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return norm_rope_backward(dout, x, weight, positions, freq, dx, dweight, T, H, d, dout_token, dout_head, x_token, x_head, dx_token, dx_head,
+                              norm_begin, norm_dim, eps, rot_begin, rot_dim, interleaved, mscale, workspace, workspace_bytes, 4, stream);
+}
+
+static int norm_rope_append(const void *q, const float *q_weight, const void *k, const float *k_weight, const void *v, const int32_t *positions,
+                            const int32_t *slots, const double *freq, void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q,
+                            int d_k, int d_v, int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token, int64_t k_head,
+                            int64_t v_token, int64_t v_head, int64_t cache_rows, int q_norm_begin, int q_norm_dim, int k_norm_begin, int k_norm_dim,
+                            float eps, int q_rot_begin, int k_rot_begin, int rot_dim, int interleaved, float mscale, int es, void *stream)
+{
+    loza::NormParams p{};
+    if (q) p.q = {{q, q_out, q_token, q_head, q_out_token, q_out_head, Hq, d_q, q_rot_begin}, q_weight, q_norm_begin, q_norm_dim, 0};
+    p.k = {{k, k_rows, k_token, k_head, (int64_t)Hkv * d_k, d_k, Hkv, d_k, k_rot_begin}, k_weight, k_norm_begin, k_norm_dim, 0};
+    p.v = v; p.v_rows = v_rows; p.v_token = v_token; p.v_head = v_head; p.d_v = d_v;
+    p.positions = positions; p.slots = slots; p.freq = freq; p.T = T; p.cache_rows = cache_rows; p.rot = rot_dim;
+    p.interleaved = interleaved != 0; p.mscale = mscale; p.eps = eps;
+    if (!slots || (q == nullptr) != (q_out == nullptr) || (v == nullptr) != (v_rows == nullptr)) return LOZA_ERR_NULL;
+    if (int rc = check_norm_call(p, (q && q_norm_dim) || k_norm_dim)) return rc;
+    if (q) { if (int rc = check_norm_heads(p.q, T, rot_dim, es, true)) return rc; }
+    if (int rc = check_norm_heads(p.k, T, rot_dim, es, false)) return rc;
+    if (k == k_rows || cache_rows < 1 || cache_rows > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(slots) & 3u) return LOZA_ERR_ALIGN;
+    if (v) {
+        if (d_v < 1 || (int64_t)Hkv * d_v > 1 << 30 || v_token < 0 || v_head < 0 || v_token > INT64_MAX / 4 / T || v_head > INT64_MAX / 4 / Hkv ||
+            v == v_rows) return LOZA_ERR_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(v_rows)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
+    }
+    return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_norm_rope_append(const void *q, const float *q_weight, const void *k, const float *k_weight, const void *v, const int32_t *positions,
+                              const int32_t *slots, const double *freq, void *q_out, void *k_rows, void *v_rows, int64_t T, int Hq, int Hkv, int d_q,
+                              int d_k, int d_v, int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token,
+                              int64_t k_head, int64_t v_token, int64_t v_head, int64_t cache_rows, int q_norm_begin, int q_norm_dim, int k_norm_begin,
+                              int k_norm_dim, float eps, int q_rot_begin, int k_rot_begin, int rot_dim, int interleaved, float mscale, void *stream)
+{
+    return norm_rope_append(q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, T, Hq, Hkv, d_q, d_k, d_v, q_token, q_head,
+                            q_out_token, q_out_head, k_token, k_head, v_token, v_head, cache_rows, q_norm_begin, q_norm_dim, k_norm_begin, k_norm_dim,
+                            eps, q_rot_begin, k_rot_begin, rot_dim, interleaved, mscale, 2, stream);
+}
+
+int loza_ssa_norm_rope_append_f32(const float *q, const float *q_weight, const float *k, const float *k_weight, const float *v, const int32_t *positions,
+                                  const int32_t *slots, const double *freq, float *q_out, float *k_rows, float *v_rows, int64_t T, int Hq, int Hkv,
+                                  int d_q, int d_k, int d_v, int64_t q_token, int64_t q_head, int64_t q_out_token, int64_t q_out_head, int64_t k_token,
+                                  int64_t k_head, int64_t v_token, int64_t v_head, int64_t cache_rows, int q_norm_begin, int q_norm_dim,
+                                  int k_norm_begin, int k_norm_dim, float eps, int q_rot_begin, int k_rot_begin, int rot_dim, int interleaved,
+                                  float mscale, void *stream)
+{
+    return norm_rope_append(q, q_weight, k, k_weight, v, positions, slots, freq, q_out, k_rows, v_rows, T, Hq, Hkv, d_q, d_k, d_v, q_token, q_head,
+                            q_out_token, q_out_head, k_token, k_head, v_token, v_head, cache_rows, q_norm_begin, q_norm_dim, k_norm_begin, k_norm_dim,
+                            eps, q_rot_begin, k_rot_begin, rot_dim, interleaved, mscale, 4, stream);
+}
+
+// ---- probabilities from logits -----------------------------------------------------------------------------
+
+// Sizes of a call that are accepted; fills in the plan.
+static int check_probs(loza::ProbsParams &p, int B, int n, int V)
+{
+    if (B < 1 || B > 65535 || n < 1 || n > LOZA_TREE_MAX_NODES || V < 1 || V > 1 << 30) return LOZA_ERR_SHAPE;
+    p.B = B; p.n = n; p.V = V;
+    loza::probs_plan(p);
+    return (int64_t)B * n * p.slices <= loza::most_workgroups(256) ? LOZA_OK : LOZA_ERR_SHAPE;
+}
+
+size_t loza_ssa_token_probs_workspace_bytes(int B, int n, int V)
+{
+    loza::ProbsParams p{};
+    return check_probs(p, B, n, V) == LOZA_OK ? (size_t)B * n * p.slices * 16 : 0;
+}
+
+static int token_probs(const void *logits, int64_t logits_row, const int32_t *tree_lens, const int32_t *tokens, const int64_t *masks, const uint16_t *seen,
+                       int64_t seen_row, const float *repetition, const float *frequency, const float *presence, const float *temperature,
+                       const int32_t *bias_tokens, const float *bias_values, int n_bias, const int32_t *allowed, float *probs, int B, int n, int V,
+                       void *workspace, size_t workspace_bytes, int es, void *stream)
+{
+    if (!logits || !probs || (tokens == nullptr) != (masks == nullptr)) return LOZA_ERR_NULL;
+    loza::ProbsParams p{};
+    if (int rc = check_probs(p, B, n, V)) return rc;
+    if (n_bias < 0 || n_bias > LOZA_MAX_BIAS) return LOZA_ERR_SHAPE;
+    if (n_bias > 0 && (!bias_tokens || !bias_values)) return LOZA_ERR_NULL;
+    if (logits_row < V || logits_row > INT64_MAX / 8 / ((int64_t)B * n)) return LOZA_ERR_SHAPE;
+    if (logits == (const void *)probs && (es != 4 || logits_row != V)) return LOZA_ERR_SHAPE;
+    if (seen && (seen_row < V || (seen_row & 7) || seen_row > INT64_MAX / 8 / B)) return LOZA_ERR_SHAPE;
+    if (!workspace || workspace_bytes < loza_ssa_token_probs_workspace_bytes(B, n, V)) return LOZA_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(logits) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
+    for (const void *ptr : {(const void *)tree_lens, (const void *)tokens, (const void *)repetition, (const void *)frequency, (const void *)presence,
+                            (const void *)temperature, (const void *)bias_tokens, (const void *)bias_values, (const void *)allowed, (const void *)probs})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(masks) & 7u) || !aligned16(seen) || !aligned16(workspace)) return LOZA_ERR_ALIGN;
+    p.logits = logits; p.logits_row = logits_row; p.tree_lens = tree_lens; p.tokens = tokens; p.masks = masks; p.seen = seen; p.seen_row = seen_row;
+    p.repetition = repetition; p.frequency = frequency; p.presence = presence; p.temperature = temperature;
+    p.bias_tokens = bias_tokens; p.bias_values = bias_values; p.n_bias = n_bias; p.allowed = allowed; p.probs = probs; p.stats = (float *)workspace;
+    return loza::launch_token_probs(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_token_probs(const void *logits, int64_t logits_row, const int32_t *tree_lens, const int32_t *tokens, const int64_t *masks,
+                         const uint16_t *seen, int64_t seen_row, const float *repetition, const float *frequency, const float *presence,
+                         const float *temperature, const int32_t *bias_tokens, const float *bias_values, int n_bias, const int32_t *allowed,
+                         float *probs, int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return token_probs(logits, logits_row, tree_lens, tokens, masks, seen, seen_row, repetition, frequency, presence, temperature, bias_tokens, bias_values,
+                       n_bias, allowed, probs, B, n, V, workspace, workspace_bytes, 2, stream);
+}
+
+int loza_ssa_token_probs_f32(const float *logits, int64_t logits_row, const int32_t *tree_lens, const int32_t *tokens, const int64_t *masks,
+                             const uint16_t *seen, int64_t seen_row, const float *repetition, const float *frequency, const float *presence,
+                             const float *temperature, const int32_t *bias_tokens, const float *bias_values, int n_bias, const int32_t *allowed,
+                             float *probs, int B, int n, int V, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return token_probs(logits, logits_row, tree_lens, tokens, masks, seen, seen_row, repetition, frequency, presence, temperature, bias_tokens, bias_values,
+                       n_bias, allowed, probs, B, n, V, workspace, workspace_bytes, 4, stream);
+}
+
+int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int32_t *lens, const int32_t *prompt_lens, const int32_t *fresh,
+                          uint16_t *seen, int64_t seen_row, int B, int n, int V, void *stream)
+{
+    if (!tokens || !lens || !seen) return LOZA_ERR_NULL;
+    if (B < 1 || B > 65535 || n < 1 || n > 1 << 30 || V < 1 || V > 1 << 30 || seen_row < V || (seen_row & 7) || seen_row > INT64_MAX / 8 / B) return LOZA_ERR_SHAPE;
+    for (const void *ptr : {(const void *)tokens, (const void *)path, (const void *)lens, (const void *)prompt_lens, (const void *)fresh})
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    if (!aligned16(seen)) return LOZA_ERR_ALIGN;
+    const loza::CountParams p{tokens, path, lens, prompt_lens, fresh, seen, seen_row, B, n, V};
+    return loza::launch_count_tokens(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+// ---- pages ------------------------------------------------------------------------------------------------------
+
+static int check_ints(std::initializer_list<const void *> pointers)
+{
+    for (const void *ptr : pointers)
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
+    return LOZA_OK;
+}
+
+int loza_ssa_pages_fork(const int32_t *from, const int32_t *cache_lens, const int32_t *held, const int32_t *trimmed, const int32_t *free_pages,
+                        const int32_t *free_count, const int32_t *shared, int32_t *block_table, int B, int64_t num_free, int64_t num_pages,
+                        int page_size, int max_pages_per_seq, int64_t sink_blocks, int64_t block, int32_t *forked, int32_t *cache_lens_after,
+                        int32_t *held_after, int32_t *trimmed_after, int32_t *copy_from, int32_t *copy_to, int32_t *copy_rows, int32_t *free_left,
+                        int32_t *shared_after, void *stream)
+{
+    if (!from || !cache_lens || !held || !free_count || !shared || !forked || !cache_lens_after || !held_after || !copy_from || !copy_to || !copy_rows ||
+        !free_left || !shared_after) return LOZA_ERR_NULL;
+    if ((trimmed == nullptr) != (trimmed_after == nullptr) || (!free_pages && num_free > 0)) return LOZA_ERR_NULL;
+    if (B < 1 || B > 65536 || num_free < 0 || num_free > 2147483647LL) return LOZA_ERR_SHAPE;   // (a workgroup adds up all requests before its own)
+    if (int rc = check_blocks(sink_blocks, 1, block)) return rc;
+    loza::ForkParams p{};
+    int64_t capacity = 0;
+    if (int rc = check_paging(Paging{block_table, num_pages, page_size, max_pages_per_seq}, &p.page_shift, &capacity)) return rc;
+    if (int rc = check_ints({from, cache_lens, held, trimmed, free_pages, free_count, shared, forked, cache_lens_after, held_after, trimmed_after, copy_from,
+                             copy_to, copy_rows, free_left, shared_after})) return rc;
+    const int64_t b4 = 4LL * B;
+    const Span arrays[] = {{forked, b4}, {cache_lens_after, b4}, {held_after, b4}, {trimmed_after, b4}, {copy_from, b4}, {copy_to, b4}, {copy_rows, b4}, {free_left, 4},
+                           {shared_after, 4 * num_pages}, {block_table, b4 * max_pages_per_seq}, {from, b4}, {cache_lens, b4}, {held, b4}, {trimmed, b4},
+                           {free_pages, 4 * num_free}, {free_count, 4}, {shared, 4 * num_pages}};
+    if (overlap(arrays, 10, 17)) return LOZA_ERR_SHAPE;
+    p.from = from; p.cache_lens = cache_lens; p.held = held; p.trimmed = trimmed; p.free_pages = free_pages; p.free_count = free_count; p.shared = shared;
+    p.block_table = block_table; p.forked = forked; p.cache_lens_after = cache_lens_after; p.held_after = held_after; p.trimmed_after = trimmed_after;
+    p.copy_from = copy_from; p.copy_to = copy_to; p.copy_rows = copy_rows; p.free_left = free_left; p.shared_after = shared_after;
+    p.B = B; p.max_pages = max_pages_per_seq; p.num_free = num_free; p.num_pages = num_pages;
+    p.sink_pages = (clamp_to(sat_mul(sink_blocks, block), capacity) + (int64_t)page_size - 1) / page_size;
+    return loza::launch_pages_fork(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+int loza_ssa_pages_copy(void *k_pages, void *v_pages, const int32_t *from, const int32_t *to, const int32_t *rows, const int32_t *count, int64_t n,
+                        int n_layers, int64_t num_pages, int page_size, int64_t k_row_bytes, int64_t v_row_bytes, void *stream)
+{
+    if (!k_pages || !from || !to) return LOZA_ERR_NULL;
+    const int64_t most = (int64_t)1 << 24;     // bytes of a row
+    if (n < 1 || n > 2147483647LL || n_layers < 1 || n_layers > 65535 || num_pages < 1 || num_pages > 2147483647LL || page_size < 1 || page_size > 1 << 20) return LOZA_ERR_SHAPE;
+    if (k_row_bytes < 16 || k_row_bytes > most || (k_row_bytes & 15)) return LOZA_ERR_SHAPE;
+    if (v_pages && (v_row_bytes < 16 || v_row_bytes > most || (v_row_bytes & 15) || v_pages == k_pages)) return LOZA_ERR_SHAPE;
+    const int64_t row = v_pages && v_row_bytes > k_row_bytes ? v_row_bytes : k_row_bytes, all = INT64_MAX / 4 / row / page_size / n_layers;
+    if (num_pages > all || n > all) return LOZA_ERR_SHAPE;
+    if (!aligned16(k_pages) || !aligned16(v_pages)) return LOZA_ERR_ALIGN;
+    if (int rc = check_ints({from, to, rows, count})) return rc;
+    const loza::CopyParams p{(char *)k_pages, (char *)v_pages, from, to, rows, count, n, num_pages, k_row_bytes, v_pages ? v_row_bytes : 0, n_layers, page_size};
+    return loza::launch_pages_copy(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+// Bytes of n 32-bit numbers, to whole 16
+static int64_t ints16(int64_t n) { return (n * 4 + 15) / 16 * 16; }
+static int64_t page_groups(int64_t num_pages) { return (num_pages + loza::kPageGroup - 1) / loza::kPageGroup; }
+
+size_t loza_ssa_pages_free_workspace_bytes(int64_t num_pages)
+{
+    if (num_pages < 1 || num_pages > 2147483647LL) return 0;
+    return (size_t)(ints16(num_pages) + ints16(page_groups(num_pages)));
+}
+
+int loza_ssa_pages_free(const int32_t *ending, const int32_t *cache_lens, const int32_t *held, const int32_t *trimmed, const int32_t *block_table,
+                        const int32_t *shared, int32_t *free_pages, const int32_t *free_count, int B, int64_t num_free, int64_t num_pages, int page_size,
+                        int max_pages_per_seq, int64_t sink_blocks, int64_t local_blocks, int64_t block, int32_t *cache_lens_after, int32_t *held_after,
+                        int32_t *trimmed_after, int32_t *free_after, int32_t *shared_after, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!cache_lens || !held || !free_pages || !free_count || !cache_lens_after || !held_after || !free_after) return LOZA_ERR_NULL;
+    if ((trimmed == nullptr) != (trimmed_after == nullptr) || (shared == nullptr) != (shared_after == nullptr)) return LOZA_ERR_NULL;
+    if (B < 1 || B > 65536 || num_free > 2147483647LL || num_free < num_pages) return LOZA_ERR_SHAPE;
+    if (int rc = check_blocks(sink_blocks, local_blocks, block)) return rc;
+    loza::FreeParams p{};
+    int64_t capacity = 0;
+    if (int rc = check_paging(Paging{block_table, num_pages, page_size, max_pages_per_seq}, &p.page_shift, &capacity)) return rc;
+    if (!workspace || workspace_bytes < loza_ssa_pages_free_workspace_bytes(num_pages)) return LOZA_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
+    if (int rc = check_ints({ending, cache_lens, held, trimmed, shared, free_pages, free_count, cache_lens_after, held_after, trimmed_after, free_after, shared_after})) return rc;
+    const int64_t b4 = 4LL * B;
+    const Span arrays[] = {{free_pages, 4 * num_free}, {cache_lens_after, b4}, {held_after, b4}, {trimmed_after, b4}, {free_after, 4}, {shared_after, 4 * num_pages},
+                           {workspace, (int64_t)loza_ssa_pages_free_workspace_bytes(num_pages)}, {ending, b4}, {cache_lens, b4}, {held, b4}, {trimmed, b4},
+                           {block_table, b4 * max_pages_per_seq}, {shared, 4 * num_pages}, {free_count, 4}};
+    if (overlap(arrays, 7, 14)) return LOZA_ERR_SHAPE;
+    const Pattern pat = block_pattern(sink_blocks, local_blocks, block, capacity + 1);       // (positions up to the capacity are asked about)
+    p.ending = ending; p.cache_lens = cache_lens; p.held = held; p.trimmed = trimmed; p.block_table = block_table; p.shared = shared;
+    p.free_count = free_count; p.free_pages = free_pages; p.cache_lens_after = cache_lens_after; p.held_after = held_after; p.trimmed_after = trimmed_after;
+    p.free_after = free_after; p.shared_after = shared_after; p.left = (int32_t *)workspace; p.freed = p.left + ints16(num_pages) / 4;
+    p.B = B; p.max_pages = max_pages_per_seq; p.window = pat.window; p.block = pat.block; p.num_free = num_free; p.num_pages = num_pages;
+    p.sink_pages = ((int64_t)pat.n_sink + page_size - 1) / page_size;
+    return loza::launch_pages_free(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
+}
+
+size_t loza_ssa_pages_compact_workspace_bytes(int64_t num_pages)
+{
+    if (num_pages < 2 || num_pages > 2147483647LL) return 0;
+    return (size_t)(ints16(num_pages) + ints16((num_pages + 31) / 32) + ints16(page_groups(num_pages)));
+}
+
+int loza_ssa_pages_compact(const int32_t *block_table, const int32_t *free_pages, const int32_t *free_count, const int32_t *shared, int B, int64_t num_free,
+                           int64_t num_pages, int max_pages_per_seq, int32_t *table_after, int32_t *free_pages_after, int32_t *free_after,
+                           int32_t *shared_after, int32_t *copy_from, int32_t *copy_to, int32_t *n_copies, void *workspace, size_t workspace_bytes,
+                           void *stream)
+{
+    if (!block_table || !free_pages || !free_count || !table_after || !free_pages_after || !free_after || !copy_from || !copy_to || !n_copies) return LOZA_ERR_NULL;
+    if ((shared == nullptr) != (shared_after == nullptr)) return LOZA_ERR_NULL;
+    if (B < 1 || B > 65536 || max_pages_per_seq < 1 || num_pages < 2 || num_pages > 2147483647LL || num_free < num_pages || num_free > 2147483647LL) return LOZA_ERR_SHAPE;
+    if (!workspace || workspace_bytes < loza_ssa_pages_compact_workspace_bytes(num_pages)) return LOZA_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
+    if (int rc = check_ints({block_table, free_pages, free_count, shared, table_after, free_pages_after, free_after, shared_after, copy_from, copy_to, n_copies})) return rc;
+    const int64_t t4 = 4LL * B * max_pages_per_seq, half = num_pages / 2 * 4;
+    const Span arrays[] = {{table_after, t4}, {free_pages_after, 4 * num_free}, {free_after, 4}, {shared_after, 4 * num_pages}, {copy_from, half}, {copy_to, half},
+                           {n_copies, 4}, {workspace, (int64_t)loza_ssa_pages_compact_workspace_bytes(num_pages)}, {block_table, t4}, {free_pages, 4 * num_free},
+                           {free_count, 4}, {shared, 4 * num_pages}};
+    if (overlap(arrays, 8, 12)) return LOZA_ERR_SHAPE;
+    loza::CompactParams p{};
+    p.block_table = block_table; p.free_pages = free_pages; p.free_count = free_count; p.shared = shared; p.table_after = table_after;
+    p.free_pages_after = free_pages_after; p.free_after = free_after; p.shared_after = shared_after; p.copy_from = copy_from; p.copy_to = copy_to;
+    p.n_copies = n_copies; p.place = (int32_t *)workspace; p.free_bits = (uint32_t *)(p.place + ints16(num_pages) / 4);
+    p.frees = (int32_t *)p.free_bits + ints16((num_pages + 31) / 32) / 4;
+    p.B = B; p.max_pages = max_pages_per_seq; p.num_free = num_free; p.num_pages = num_pages;
+    return loza::launch_pages_compact(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }
 
 }  // extern "C"

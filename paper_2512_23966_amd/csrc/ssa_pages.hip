@@ -1,0 +1,389 @@
+// Pages of a cache beyond what a step needs (gfx950): shared with forks, copied, given back, moved to the front of the pool.
+//
+// A page belongs to the requests whose rows of the block table name it: one, and as many more as shared[page] says. Numbers of holders
+// are changed by integer atomics, whose order does not show; lists are written in the order of requests or of page numbers, by counting
+// what comes before. What bounds all of it but the copies: the latency of a few launches and of the loads in them that wait for each other.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ssa_device.h"
+#include "ssa_step.h"
+
+namespace loza {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ T wave_total(T x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+
+__device__ __forceinline__ int64_t valid_count(const int32_t *count, int64_t num_free)
+{
+    const int64_t c = count[0];
+    return c < 0 ? 0 : c < num_free ? c : num_free;
+}
+
+// ---- forks ---------------------------------------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void copy_ints_kernel(const int32_t *__restrict__ from, int32_t *__restrict__ to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from[i];
+}
+
+// What request b asks for: to become a copy of `source`, whose cache has `rows` rows
+struct Fork {
+    int source;
+    int64_t rows;
+    bool fits;
+    int need;                      // pages: 1 for a page that is started and not full
+};
+__device__ __forceinline__ Fork fork_of(const ForkParams &p, int b)
+{
+    Fork f;
+    f.source = p.from[b];
+    f.fits = f.source >= 0 && f.source < p.B && p.cache_lens[b] == 0 && p.held[b] == 0;
+    f.rows = f.fits ? p.cache_lens[f.source] : 0;
+    if (f.rows < 0 || f.rows > (int64_t)p.max_pages << p.page_shift) f.fits = false;
+    f.need = f.fits && (f.rows & (((int64_t)1 << p.page_shift) - 1)) != 0;
+    return f;
+}
+
+// A workgroup a request. Pages are dealt out in the order of the requests: each adds up what those before its own need.
+__global__ __launch_bounds__(256) void pages_fork_kernel(const ForkParams p)
+{
+    __shared__ int64_t s_sum[4];
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int64_t count = valid_count(p.free_count, p.num_free);
+    int64_t before = 0;
+    const int upto = b == 0 ? p.B : b;             // (the first one adds up all, for what is left)
+    for (int i = tid; i < upto; i += 256) before += fork_of(p, i).need;
+    before = wave_total(before);
+    if ((tid & 63) == 0) s_sum[tid >> 6] = before;
+    __syncthreads();
+    before = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    if (b == 0) {
+        if (tid == 0) p.free_left[0] = (int32_t)(count - (before < count ? before : count));
+        before = 0;
+    }
+    const Fork f = fork_of(p, b);
+    const bool ok = f.fits && (f.need == 0 || before < count);
+    const int64_t full = ok ? f.rows >> p.page_shift : 0;
+    int64_t first = 0;                             // pages of the source from here on, and those of the sink, are still its own
+    if (p.trimmed && ok) first = p.trimmed[f.source];
+    int32_t *to = p.block_table + (int64_t)b * p.max_pages;
+    const int32_t *from = p.block_table + (int64_t)(ok ? f.source : b) * p.max_pages;
+    for (int64_t i = tid; i < full; i += 256) {
+        const int page = from[i];
+        to[i] = page;
+        if ((i < p.sink_pages || i >= first) && page >= 0 && page < p.num_pages) atomicAdd(&p.shared_after[page], 1);
+    }
+    if (tid != 0) return;
+    const bool started = ok && f.need;
+    int source = -1, target = -1;
+    if (started) {
+        source = from[full];
+        target = p.free_pages[count - 1 - before];
+        to[full] = target;
+    }
+    p.forked[b] = ok;
+    p.cache_lens_after[b] = ok ? (int32_t)f.rows : p.cache_lens[b];
+    p.held_after[b] = ok ? (int32_t)(full + f.need) : p.held[b];
+    if (p.trimmed) p.trimmed_after[b] = ok ? (int32_t)first : p.trimmed[b];
+    p.copy_from[b] = source;
+    p.copy_to[b] = target;
+    p.copy_rows[b] = started ? (int32_t)(f.rows & (((int64_t)1 << p.page_shift) - 1)) : 0;
+}
+
+// ---- copies ---------------------------------------------------------------------------------------------
+
+// Workgroups take pieces of 16 KB of the pages of all layers in turn.
+constexpr int kPiece = 256 * 16 * 4;
+
+__global__ __launch_bounds__(256) void pages_copy_kernel(const CopyParams p)
+{
+    int64_t n = p.n;
+    if (p.count) {
+        const int64_t c = p.count[0];
+        n = c < 0 ? 0 : c < n ? c : n;
+    }
+    const int64_t k_bytes = p.k_row * p.page_size, v_bytes = p.v_row * p.page_size;
+    const int k_pieces = (int)((k_bytes + kPiece - 1) / kPiece), v_pieces = (int)((v_bytes + kPiece - 1) / kPiece), pieces = k_pieces + v_pieces;
+    const int64_t items = n * p.layers * pieces;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t il = item / pieces, i = il / p.layers, layer = il - i * p.layers;
+        const int piece = (int)(item - il * pieces);
+        const int64_t from = p.from[i], to = p.to[i];
+        if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages || from == to) continue;
+        int64_t rows = p.rows ? p.rows[i] : p.page_size;
+        rows = rows < 0 ? 0 : rows < p.page_size ? rows : p.page_size;
+        const bool values = piece >= k_pieces;
+        const int64_t page_bytes = values ? v_bytes : k_bytes, bytes = rows * (values ? p.v_row : p.k_row);
+        char *pages = (values ? p.v_pages : p.k_pages) + layer * p.num_pages * page_bytes;
+        const int64_t at = (int64_t)(piece - (values ? k_pieces : 0)) * kPiece + threadIdx.x * 16;
+        const char *x = pages + from * page_bytes;
+        char *y = pages + to * page_bytes;
+        u32x4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at + k * 4096 < bytes) v[k] = *(const u32x4 *)(x + at + k * 4096);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at + k * 4096 < bytes) *(u32x4 *)(y + at + k * 4096) = v[k];
+    }
+}
+
+// ---- pages given back ----------------------------------------------------------------------------------
+//
+// left[page] starts as the number of holders beyond the first; each entry that is given up takes one off, and the one that finds 0 was
+// the last. Freed pages go to the list by number: groups of kGroup pages count theirs, and each then knows where its own begin.
+
+__global__ __launch_bounds__(256) void free_start_kernel(const FreeParams p)
+{
+    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.num_pages; i += (int64_t)gridDim.x * 256) p.left[i] = p.shared ? p.shared[i] : 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups; i += (int64_t)gridDim.x * 256) p.freed[i] = 0;
+}
+
+__global__ __launch_bounds__(256) void free_mark_kernel(const FreeParams p)
+{
+    const int b = blockIdx.x;
+    const int64_t size = (int64_t)1 << p.page_shift, len = p.cache_lens[b], held = p.held[b];
+    const int trimmed = p.trimmed ? p.trimmed[b] : 0;
+    const bool fits = len >= 0 && len <= (int64_t)p.max_pages * size && held >= 0 && held <= p.max_pages;
+    const bool ends = fits && p.ending && p.ending[b] != 0;
+    const int64_t used = (len + size - 1) >> p.page_shift, have = held > used ? held : used;
+    int64_t first = trimmed > p.sink_pages ? trimmed : p.sink_pages;     // entries [0, sink_pages) and [first, have) are the request's
+    int64_t upto = first;                                                // entries [first, upto) are given up, and the sink's where the request ends
+    if (ends) {
+        upto = have;
+    } else if (fits && p.trimmed) {
+        const int64_t seen = (int64_t)window_begin_of((int)len, p.window, p.block) >> p.page_shift;
+        upto = seen > first ? seen : first;
+    }
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        p.cache_lens_after[b] = ends ? 0 : (int32_t)len;
+        p.held_after[b] = ends ? 0 : (int32_t)held;
+        if (p.trimmed) p.trimmed_after[b] = ends ? 0 : upto > p.sink_pages ? (int32_t)(upto > trimmed ? upto : trimmed) : trimmed;
+    }
+    if (!fits) return;
+    const int32_t *table = p.block_table + (int64_t)b * p.max_pages;
+    const int64_t sink = ends ? (p.sink_pages < have ? p.sink_pages : have) : 0;
+    const int64_t step = (int64_t)gridDim.y * 256, me = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    auto give = [&](int64_t i) {
+        const int page = table[i];
+        if (page < 0 || page >= p.num_pages) return;
+        if (atomicSub(&p.left[page], 1) == 0) atomicAdd(&p.freed[page / kPageGroup], 1);
+    };
+    for (int64_t i = me; i < sink; i += step) give(i);
+    for (int64_t i = first + me; i < upto && i < have; i += step) give(i);
+}
+
+// Sum of the groups' numbers before group g, and of all, by a workgroup of 1,024
+__device__ __forceinline__ void sum_groups(const int32_t *numbers, int64_t groups, int64_t g, int64_t &before, int64_t &all, int64_t *lds)
+{
+    int64_t a = 0, t = 0;
+    for (int64_t i = threadIdx.x; i < groups; i += 1024) {
+        t += numbers[i];
+        a += i < g ? numbers[i] : 0;
+    }
+    a = wave_total(a);
+    t = wave_total(t);
+    if ((threadIdx.x & 63) == 0) {
+        lds[threadIdx.x >> 6] = a;
+        lds[16 + (threadIdx.x >> 6)] = t;
+    }
+    __syncthreads();
+    before = all = 0;
+    for (int i = 0; i < 16; ++i) {
+        before += lds[i];
+        all += lds[16 + i];
+    }
+    __syncthreads();
+}
+
+// Numbers before this thread's in a workgroup of 1,024 (each 0 .. 4)
+__device__ __forceinline__ int scan_before(int x, int32_t *lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += up;
+    }
+    if (lane == 63) lds[wave] = sum;
+    __syncthreads();
+    int before = sum - x;
+    for (int i = 0; i < wave; ++i) before += lds[i];
+    __syncthreads();
+    return before;
+}
+
+// A workgroup a group of kPageGroup pages, 4 a thread
+__global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
+{
+    __shared__ int64_t s_sum[32];
+    __shared__ int32_t s_scan[16];
+    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup, count = valid_count(p.free_count, p.num_free);
+    int64_t before, all;
+    sum_groups(p.freed, groups, blockIdx.x, before, all, s_sum);
+    const int64_t page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4;
+    int left[4], mine = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        left[k] = page0 + k < p.num_pages ? p.left[page0 + k] : 0;
+        mine += left[k] < 0;
+        if (p.shared && page0 + k < p.num_pages) p.shared_after[page0 + k] = left[k] < 0 ? 0 : left[k];
+    }
+    int64_t at = count + before + scan_before(mine, s_scan);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (left[k] < 0) {
+            if (at < p.num_free) p.free_pages[at] = (int32_t)(page0 + k);
+            ++at;
+        }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.free_after[0] = (int32_t)(count + all < p.num_free ? count + all : p.num_free);
+}
+
+// ---- the pool tidied ------------------------------------------------------------------------------------
+//
+// With u pages in use, those from u on move to the free ones below u, each list by number: the i-th to the i-th.
+
+__global__ __launch_bounds__(256) void compact_start_kernel(const CompactParams p)
+{
+    const int64_t words = (p.num_pages + 31) / 32, groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p.free_bits[i] = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups; i += (int64_t)gridDim.x * 256) p.frees[i] = 0;
+}
+
+__global__ __launch_bounds__(256) void compact_mark_kernel(const CompactParams p)
+{
+    const int64_t count = valid_count(p.free_count, p.num_free);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        const int page = p.free_pages[i];
+        if (page < 0 || page >= p.num_pages) continue;
+        const uint32_t bit = 1u << (page & 31);
+        if (!(atomicOr(&p.free_bits[page >> 5], bit) & bit)) atomicAdd(&p.frees[page / kPageGroup], 1);
+    }
+}
+
+// A workgroup a group of pages: the lists of copies, each page's place in them, and the new free list
+__global__ __launch_bounds__(1024) void compact_lists_kernel(const CompactParams p)
+{
+    __shared__ int64_t s_sum[32];
+    __shared__ int32_t s_scan[16];
+    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
+    int64_t before, all, holes, unused;
+    sum_groups(p.frees, groups, blockIdx.x, before, all, s_sum);
+    const int64_t used = p.num_pages - all;
+    // free pages below `used`: of the groups before its own, and of its own
+    sum_groups(p.frees, groups, used / kPageGroup, holes, unused, s_sum);
+    {
+        const int64_t w0 = used / kPageGroup * (kPageGroup / 32), w = w0 + threadIdx.x;
+        int bits = 0;
+        if (threadIdx.x < kPageGroup / 32 && w * 32 < used) {
+            uint32_t x = p.free_bits[w];
+            if (w * 32 + 32 > used) x &= (1u << (used - w * 32)) - 1;
+            bits = __popc(x);
+        }
+        int64_t sum = wave_total((int64_t)bits);
+        if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        for (int i = 0; i < kPageGroup / 32 / 64; ++i) holes += s_sum[i];
+        __syncthreads();
+    }
+    const int64_t page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4, most = p.num_pages / 2;
+    const uint32_t bits = page0 < p.num_pages ? p.free_bits[page0 >> 5] >> (page0 & 31) & 15u : 0u;
+    int64_t frees = before + scan_before(__popc(bits), s_scan);         // before page0 + k
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t page = page0 + k;
+        if (page >= p.num_pages) break;
+        const bool is_free = bits >> k & 1;
+        if (is_free && page < used) {
+            p.copy_to[frees] = (int32_t)page;
+            p.place[page] = (int32_t)frees;
+        } else if (!is_free && page >= used) {
+            const int64_t i = page - frees - (used - holes);
+            p.copy_from[i] = (int32_t)page;
+            p.place[page] = (int32_t)i;
+        }
+        if (page >= holes && page < most) p.copy_from[page] = p.copy_to[page] = -1;
+        frees += is_free;
+    }
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < p.num_free; i += (int64_t)gridDim.x * 1024)
+        p.free_pages_after[i] = i < all ? (int32_t)(p.num_pages - 1 - i) : -1;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        p.free_after[0] = (int32_t)all;
+        p.n_copies[0] = (int32_t)holes;
+    }
+}
+
+__global__ __launch_bounds__(256) void compact_rename_kernel(const CompactParams p)
+{
+    const int64_t used = p.num_pages - p.free_after[0], entries = (int64_t)p.B * p.max_pages, step = (int64_t)gridDim.x * 256;
+    auto is_free = [&](int64_t page) { return p.free_bits[page >> 5] >> (page & 31) & 1u; };
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += step) {
+        const int page = p.block_table[i];
+        p.table_after[i] = page >= used && page < p.num_pages && !is_free(page) ? p.copy_to[p.place[page]] : page;
+    }
+    if (p.shared == nullptr) return;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.num_pages; i += step)
+        p.shared_after[i] = i >= used ? 0 : p.shared[is_free(i) ? p.copy_from[p.place[i]] : i];
+}
+
+unsigned blocks_for(int64_t n, int threads, int64_t most)
+{
+    const int64_t b = (n + threads - 1) / threads;
+    return (unsigned)(b < 1 ? 1 : b < most ? b : most);
+}
+
+}  // namespace
+
+hipError_t launch_pages_fork(const ForkParams &p, hipStream_t stream)
+{
+    hipLaunchKernelGGL(copy_ints_kernel, dim3(blocks_for(p.num_pages, 256, 1024)), dim3(256), 0, stream, p.shared, p.shared_after, p.num_pages);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)p.B), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const CopyParams &p, hipStream_t stream)
+{
+    const int64_t pieces = (p.k_row * p.page_size + kPiece - 1) / kPiece + (p.v_row * p.page_size + kPiece - 1) / kPiece;
+    // (step by step: the product of all may pass 64 bits)
+    int64_t items = p.n < 2048 ? p.n : 2048;
+    items = items * p.layers < 2048 ? items * p.layers : 2048;
+    items = items * pieces < 2048 ? items * pieces : 2048;
+    hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)items), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_free(const FreeParams &p, hipStream_t stream)
+{
+    hipLaunchKernelGGL(free_start_kernel, dim3(blocks_for(p.num_pages, 256, 1024)), dim3(256), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(free_mark_kernel, dim3((unsigned)p.B, blocks_for(p.max_pages, 1024, 16)), dim3(256), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(free_append_kernel, dim3((unsigned)((p.num_pages + kPageGroup - 1) / kPageGroup)), dim3(1024), 0, stream, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const CompactParams &p, hipStream_t stream)
+{
+    hipLaunchKernelGGL(compact_start_kernel, dim3(blocks_for(p.num_pages / 32 + 1, 256, 256)), dim3(256), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(compact_mark_kernel, dim3(blocks_for(p.num_free, 256, 1024)), dim3(256), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(compact_lists_kernel, dim3((unsigned)((p.num_pages + kPageGroup - 1) / kPageGroup)), dim3(1024), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const int64_t entries = (int64_t)p.B * p.max_pages;
+    hipLaunchKernelGGL(compact_rename_kernel, dim3(blocks_for(entries > p.num_pages ? entries : p.num_pages, 1024, 2048)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace loza
