@@ -664,7 +664,7 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
  *   tree_lens [B] int32 or NULL (n rows each): rows r >= tree_lens[b] of probs are left as they are, and their logits are not read
  *   tokens [B, n] int32, masks [B, n] int64, or both NULL: a row's own path (loza_ssa_step_tables makes the masks): the tokens of the nodes in masks[b, r],
  *           those below tree_lens[b], were said as well, each once a node
- *   seen [B] rows, seen_row elements apart (a multiple of 8, >= V; 16-byte aligned), or NULL: what was said before the path (loza_ssa_count_tokens):
+ *   seen [B] rows, seen_row elements apart (a multiple of 8, >= V, < 2^31; 16-byte aligned), or NULL: what was said before the path (loza_ssa_count_tokens):
  *           bit 15 says that the token occurs in the prompt, the others how often it was said
  *   repetition (> 0; NULL: 1), frequency, presence (NULL: 0), temperature (NULL: 1) [B] fp32
  *   bias_tokens [B, n_bias] int32, bias_values [B, n_bias] fp32 (n_bias <= LOZA_MAX_BIAS; tokens outside [0, V) are skipped, those of one token add up in order)
@@ -672,7 +672,7 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
  *   workspace: loza_ssa_token_probs_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
  * Token x with logit l, said c times: l / repetition if l > 0, l repetition otherwise, where it was said or occurs in the prompt; less frequency c and
  * (c > 0) presence; plus its bias; each operation rounded to fp32. Tokens that are not allowed, whatever their logits, and those whose result is a NaN, weigh
- * nothing. probs = exp((l - max) / temperature) / sum; where the temperature is not in [2^-126, 2^126] (0: greedy): 1 at the first of the largest. A row in
+ * nothing. probs = exp((l - max) / temperature) / sum; where the temperature is not in [2^-100, 2^100] (0: greedy): 1 at the first of the largest. A row in
  * which nothing weighs is all 0 (loza_ssa_verify_tree then has no next token). Logits of +infinity share a row among them.
  * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30, as many rows as a launch takes. Sums in fp32, always in the same order.
  */

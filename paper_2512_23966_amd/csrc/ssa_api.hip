@@ -1621,6 +1621,8 @@ int loza_ssa_norm_rope_append_f32(const float *q, const float *q_weight, const f
 
 // ---- probabilities from logits -----------------------------------------------------------------------------
 
+constexpr int64_t kMostSeen = 2147483640;      // elements of a row of the record (their numbers are 32-bit)
+
 // Sizes of a call that are accepted; fills in the plan.
 static int check_probs(loza::ProbsParams &p, int B, int n, int V)
 {
@@ -1648,7 +1650,7 @@ static int token_probs(const void *logits, int64_t logits_row, const int32_t *tr
     if (n_bias > 0 && (!bias_tokens || !bias_values)) return LOZA_ERR_NULL;
     if (logits_row < V || logits_row > INT64_MAX / 8 / ((int64_t)B * n)) return LOZA_ERR_SHAPE;
     if (logits == (const void *)probs && (es != 4 || logits_row != V)) return LOZA_ERR_SHAPE;
-    if (seen && (seen_row < V || (seen_row & 7) || seen_row > INT64_MAX / 8 / B)) return LOZA_ERR_SHAPE;
+    if (seen && (seen_row < V || (seen_row & 7) || seen_row > kMostSeen)) return LOZA_ERR_SHAPE;
     if (!workspace || workspace_bytes < loza_ssa_token_probs_workspace_bytes(B, n, V)) return LOZA_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(logits) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
     for (const void *ptr : {(const void *)tree_lens, (const void *)tokens, (const void *)repetition, (const void *)frequency, (const void *)presence,
@@ -1683,7 +1685,7 @@ int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int3
                           uint16_t *seen, int64_t seen_row, int B, int n, int V, void *stream)
 {
     if (!tokens || !lens || !seen) return LOZA_ERR_NULL;
-    if (B < 1 || B > 65535 || n < 1 || n > 1 << 30 || V < 1 || V > 1 << 30 || seen_row < V || (seen_row & 7) || seen_row > INT64_MAX / 8 / B) return LOZA_ERR_SHAPE;
+    if (B < 1 || B > 65535 || n < 1 || n > 1 << 30 || V < 1 || V > 1 << 30 || seen_row < V || (seen_row & 7) || seen_row > kMostSeen) return LOZA_ERR_SHAPE;
     for (const void *ptr : {(const void *)tokens, (const void *)path, (const void *)lens, (const void *)prompt_lens, (const void *)fresh})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if (!aligned16(seen)) return LOZA_ERR_ALIGN;
@@ -1747,12 +1749,11 @@ int loza_ssa_pages_copy(void *k_pages, void *v_pages, const int32_t *from, const
 
 // Bytes of n 32-bit numbers, to whole 16
 static int64_t ints16(int64_t n) { return (n * 4 + 15) / 16 * 16; }
-static int64_t page_groups(int64_t num_pages) { return (num_pages + loza::kPageGroup - 1) / loza::kPageGroup; }
 
 size_t loza_ssa_pages_free_workspace_bytes(int64_t num_pages)
 {
     if (num_pages < 1 || num_pages > 2147483647LL) return 0;
-    return (size_t)(ints16(num_pages) + ints16(page_groups(num_pages)));
+    return (size_t)(ints16(num_pages) + ints16((num_pages + 31) / 32));
 }
 
 int loza_ssa_pages_free(const int32_t *ending, const int32_t *cache_lens, const int32_t *held, const int32_t *trimmed, const int32_t *block_table,
@@ -1778,7 +1779,7 @@ int loza_ssa_pages_free(const int32_t *ending, const int32_t *cache_lens, const 
     const Pattern pat = block_pattern(sink_blocks, local_blocks, block, capacity + 1);       // (positions up to the capacity are asked about)
     p.ending = ending; p.cache_lens = cache_lens; p.held = held; p.trimmed = trimmed; p.block_table = block_table; p.shared = shared;
     p.free_count = free_count; p.free_pages = free_pages; p.cache_lens_after = cache_lens_after; p.held_after = held_after; p.trimmed_after = trimmed_after;
-    p.free_after = free_after; p.shared_after = shared_after; p.left = (int32_t *)workspace; p.freed = p.left + ints16(num_pages) / 4;
+    p.free_after = free_after; p.shared_after = shared_after; p.left = (int32_t *)workspace; p.freed = (uint32_t *)(p.left + ints16(num_pages) / 4);
     p.B = B; p.max_pages = max_pages_per_seq; p.window = pat.window; p.block = pat.block; p.num_free = num_free; p.num_pages = num_pages;
     p.sink_pages = ((int64_t)pat.n_sink + page_size - 1) / page_size;
     return loza::launch_pages_free(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
@@ -1787,7 +1788,7 @@ int loza_ssa_pages_free(const int32_t *ending, const int32_t *cache_lens, const 
 size_t loza_ssa_pages_compact_workspace_bytes(int64_t num_pages)
 {
     if (num_pages < 2 || num_pages > 2147483647LL) return 0;
-    return (size_t)(ints16(num_pages) + ints16((num_pages + 31) / 32) + ints16(page_groups(num_pages)));
+    return (size_t)(ints16(num_pages) + ints16((num_pages + 31) / 32));
 }
 
 int loza_ssa_pages_compact(const int32_t *block_table, const int32_t *free_pages, const int32_t *free_count, const int32_t *shared, int B, int64_t num_free,
@@ -1810,7 +1811,6 @@ int loza_ssa_pages_compact(const int32_t *block_table, const int32_t *free_pages
     p.block_table = block_table; p.free_pages = free_pages; p.free_count = free_count; p.shared = shared; p.table_after = table_after;
     p.free_pages_after = free_pages_after; p.free_after = free_after; p.shared_after = shared_after; p.copy_from = copy_from; p.copy_to = copy_to;
     p.n_copies = n_copies; p.place = (int32_t *)workspace; p.free_bits = (uint32_t *)(p.place + ints16(num_pages) / 4);
-    p.frees = (int32_t *)p.free_bits + ints16((num_pages + 31) / 32) / 4;
     p.B = B; p.max_pages = max_pages_per_seq; p.num_free = num_free; p.num_pages = num_pages;
     return loza::launch_pages_compact(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }

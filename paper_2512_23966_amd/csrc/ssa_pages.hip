@@ -139,13 +139,14 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const CopyParams p)
 // ---- pages given back ----------------------------------------------------------------------------------
 //
 // left[page] starts as the number of holders beyond the first; each entry that is given up takes one off, and the one that finds 0 was
-// the last. Freed pages go to the list by number: groups of kGroup pages count theirs, and each then knows where its own begin.
+// the last and sets the page's bit. Freed pages go to the list by number: the workgroup of kPageGroup pages counts the bits before its own. (A number
+// of freed pages for each group, added to by atomics, had the adds to one address wait for each other: 48 us for 10,000 pages.)
 
 __global__ __launch_bounds__(256) void free_start_kernel(const FreeParams p)
 {
-    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
+    const int64_t words = (p.num_pages + 31) / 32;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.num_pages; i += (int64_t)gridDim.x * 256) p.left[i] = p.shared ? p.shared[i] : 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups; i += (int64_t)gridDim.x * 256) p.freed[i] = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p.freed[i] = 0;
 }
 
 __global__ __launch_bounds__(256) void free_mark_kernel(const FreeParams p)
@@ -176,33 +177,35 @@ __global__ __launch_bounds__(256) void free_mark_kernel(const FreeParams p)
     auto give = [&](int64_t i) {
         const int page = table[i];
         if (page < 0 || page >= p.num_pages) return;
-        if (atomicSub(&p.left[page], 1) == 0) atomicAdd(&p.freed[page / kPageGroup], 1);
+        if (atomicSub(&p.left[page], 1) == 0) atomicOr(&p.freed[page >> 5], 1u << (page & 31));
     };
     for (int64_t i = me; i < sink; i += step) give(i);
     for (int64_t i = first + me; i < upto && i < have; i += step) give(i);
 }
 
-// Sum of the groups' numbers before group g, and of all, by a workgroup of 1,024
-__device__ __forceinline__ void sum_groups(const int32_t *numbers, int64_t groups, int64_t g, int64_t &before, int64_t &all, int64_t *lds)
+// How many of the bits below `limit` are set, by a workgroup of 1,024
+__device__ __forceinline__ int64_t bits_below(const uint32_t *bits, int64_t limit, int64_t *lds)
 {
-    int64_t a = 0, t = 0;
-    for (int64_t i = threadIdx.x; i < groups; i += 1024) {
-        t += numbers[i];
-        a += i < g ? numbers[i] : 0;
+    int64_t sum = 0;
+    const int64_t words = limit / 32;
+    for (int64_t i = threadIdx.x * 4; i + 4 <= words; i += 4096) {
+        const u32x4 x = *(const u32x4 *)(bits + i);
+        sum += __popc(x[0]) + __popc(x[1]) + __popc(x[2]) + __popc(x[3]);
     }
-    a = wave_total(a);
-    t = wave_total(t);
-    if ((threadIdx.x & 63) == 0) {
-        lds[threadIdx.x >> 6] = a;
-        lds[16 + (threadIdx.x >> 6)] = t;
+    if (threadIdx.x < 4) {                                           // up to three whole words, and a part of one
+        const int64_t i = words / 4 * 4 + threadIdx.x;
+        if (i * 32 < limit) {
+            const uint32_t x = bits[i];
+            sum += __popc(i < words ? x : x & ((1u << (limit & 31)) - 1));
+        }
     }
+    sum = wave_total(sum);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
     __syncthreads();
-    before = all = 0;
-    for (int i = 0; i < 16; ++i) {
-        before += lds[i];
-        all += lds[16 + i];
-    }
+    sum = 0;
+    for (int i = 0; i < 16; ++i) sum += lds[i];
     __syncthreads();
+    return sum;
 }
 
 // Numbers before this thread's in a workgroup of 1,024 (each 0 .. 4)
@@ -226,11 +229,9 @@ __device__ __forceinline__ int scan_before(int x, int32_t *lds)
 // A workgroup a group of kPageGroup pages, 4 a thread
 __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
 {
-    __shared__ int64_t s_sum[32];
+    __shared__ int64_t s_sum[16];
     __shared__ int32_t s_scan[16];
-    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup, count = valid_count(p.free_count, p.num_free);
-    int64_t before, all;
-    sum_groups(p.freed, groups, blockIdx.x, before, all, s_sum);
+    const int64_t count = valid_count(p.free_count, p.num_free), before = bits_below(p.freed, (int64_t)blockIdx.x * kPageGroup, s_sum);
     const int64_t page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4;
     int left[4], mine = 0;
 #pragma unroll
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
             if (at < p.num_free) p.free_pages[at] = (int32_t)(page0 + k);
             ++at;
         }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.free_after[0] = (int32_t)(count + all < p.num_free ? count + all : p.num_free);
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 1023) p.free_after[0] = (int32_t)(at < p.num_free ? at : p.num_free);   // (behind the last one's own)
 }
 
 // ---- the pool tidied ------------------------------------------------------------------------------------
@@ -255,9 +256,8 @@ __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
 
 __global__ __launch_bounds__(256) void compact_start_kernel(const CompactParams p)
 {
-    const int64_t words = (p.num_pages + 31) / 32, groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
+    const int64_t words = (p.num_pages + 31) / 32;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p.free_bits[i] = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups; i += (int64_t)gridDim.x * 256) p.frees[i] = 0;
 }
 
 __global__ __launch_bounds__(256) void compact_mark_kernel(const CompactParams p)
@@ -266,36 +266,17 @@ __global__ __launch_bounds__(256) void compact_mark_kernel(const CompactParams p
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
         const int page = p.free_pages[i];
         if (page < 0 || page >= p.num_pages) continue;
-        const uint32_t bit = 1u << (page & 31);
-        if (!(atomicOr(&p.free_bits[page >> 5], bit) & bit)) atomicAdd(&p.frees[page / kPageGroup], 1);
+        atomicOr(&p.free_bits[page >> 5], 1u << (page & 31));
     }
 }
 
 // A workgroup a group of pages: the lists of copies, each page's place in them, and the new free list
 __global__ __launch_bounds__(1024) void compact_lists_kernel(const CompactParams p)
 {
-    __shared__ int64_t s_sum[32];
+    __shared__ int64_t s_sum[16];
     __shared__ int32_t s_scan[16];
-    const int64_t groups = (p.num_pages + kPageGroup - 1) / kPageGroup;
-    int64_t before, all, holes, unused;
-    sum_groups(p.frees, groups, blockIdx.x, before, all, s_sum);
-    const int64_t used = p.num_pages - all;
-    // free pages below `used`: of the groups before its own, and of its own
-    sum_groups(p.frees, groups, used / kPageGroup, holes, unused, s_sum);
-    {
-        const int64_t w0 = used / kPageGroup * (kPageGroup / 32), w = w0 + threadIdx.x;
-        int bits = 0;
-        if (threadIdx.x < kPageGroup / 32 && w * 32 < used) {
-            uint32_t x = p.free_bits[w];
-            if (w * 32 + 32 > used) x &= (1u << (used - w * 32)) - 1;
-            bits = __popc(x);
-        }
-        int64_t sum = wave_total((int64_t)bits);
-        if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        for (int i = 0; i < kPageGroup / 32 / 64; ++i) holes += s_sum[i];
-        __syncthreads();
-    }
+    const int64_t before = bits_below(p.free_bits, (int64_t)blockIdx.x * kPageGroup, s_sum), all = bits_below(p.free_bits, p.num_pages, s_sum);
+    const int64_t used = p.num_pages - all, holes = bits_below(p.free_bits, used, s_sum);
     const int64_t page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4, most = p.num_pages / 2;
     const uint32_t bits = page0 < p.num_pages ? p.free_bits[page0 >> 5] >> (page0 & 31) & 15u : 0u;
     int64_t frees = before + scan_before(__popc(bits), s_scan);         // before page0 + k

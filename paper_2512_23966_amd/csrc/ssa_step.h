@@ -136,7 +136,8 @@ constexpr int kPageGroup = 4096;      // pages a workgroup counts
 struct FreeParams {
     const int32_t *ending, *cache_lens, *held, *trimmed, *block_table, *shared, *free_count;
     int32_t *free_pages, *cache_lens_after, *held_after, *trimmed_after, *free_after, *shared_after;
-    int32_t *left, *freed;        // workspace: [num_pages], [groups of pages]
+    int32_t *left;                // workspace: [num_pages], and a bit a page
+    uint32_t *freed;
     int B, page_shift, max_pages, window, block;
     int64_t num_free, num_pages, sink_pages;
 };
@@ -145,7 +146,7 @@ hipError_t launch_pages_free(const FreeParams &p, hipStream_t stream);
 struct CompactParams {
     const int32_t *block_table, *free_pages, *free_count, *shared;
     int32_t *table_after, *free_pages_after, *free_after, *shared_after, *copy_from, *copy_to, *n_copies;
-    int32_t *place, *frees;       // workspace: [num_pages], [groups of pages], and a bit a page
+    int32_t *place;               // workspace: [num_pages], and a bit a page
     uint32_t *free_bits;
     int B, max_pages;
     int64_t num_free, num_pages;

@@ -96,14 +96,14 @@ def changed_logits(logits, said, occurs, rep, fre, pre, bias, allowed):
 
 
 def probabilities(l, temperature):
-    """From the changed logits of a row, in 64 bits, and their bound: the difference to the largest, its product with 1 / T and the exponential are off by
-    2^-24 of |l - max| / T and by 4 units; sums of V positive terms over at least 256 threads of 8 each, whose reference moves once a unit at most (4 units each
-    time), by V / 256 + 4 V / 2048 + 100."""
+    """From the changed logits of a row, in 64 bits, and their bound: the difference to the largest is off by 2^-24 of |l - max| / T, the rest of a token's own
+    weight by 8 units; in the sum, the product with 1 / T and that number's own rounding are off by as much each again, 3 of the weighted mean of |l - max| / T; sums
+    of V positive terms over at least 256 threads of 8 each, whose reference moves once a unit at most (4 units each time), by V / 256 + 4 V / 2048 + 100."""
     l = l.astype(np.float64)
     top = l.max()
     if top == -np.inf:
         return np.zeros(len(l)), np.zeros(len(l))
-    if not 2.0 ** -126 <= temperature <= 2.0 ** 126:
+    if not 2.0 ** -100 <= temperature <= 2.0 ** 100:
         p = np.zeros(len(l))
         p[int(np.argmax(l))] = 1.0
         return p, np.zeros(len(l))
@@ -113,7 +113,7 @@ def probabilities(l, temperature):
     p = e / e.sum()
     n = len(l)
     live = np.where(np.isfinite(d), np.abs(d), 0.0)
-    units = live + (e * live).sum() / e.sum() + 8 + n / 256 + 4 * n / 2048 + 100
+    units = live + 3 * (e * live).sum() / e.sum() + 8 + n / 256 + 4 * n / 2048 + 100
     return p, units * U * p + 1e-37
 
 

@@ -172,10 +172,10 @@ def test_pages_compact_refusals():
         a = {name: (i + 1) * A for i, name in enumerate(ins)}
         a.update(B=2, num_free=100, num_pages=100, most=16)
         a.update({name: (i + 20) * A for i, name in enumerate(outs)})
-        a.update(ws=40 * A, nb=432)
+        a.update(ws=40 * A, nb=416)
         a.update(k)
         return B.lib().loza_ssa_pages_compact(*a.values(), None)
-    assert loza.loza_ssa_pages_compact_workspace_bytes(100) == 432 and loza.loza_ssa_pages_compact_workspace_bytes(1) == 0
+    assert loza.loza_ssa_pages_compact_workspace_bytes(100) == 416 and loza.loza_ssa_pages_compact_workspace_bytes(1) == 0
     for name in ins + outs:
         assert call(**{name: None}) == ERR_NULL, name
     for bad in (dict(B=0), dict(B=65537), dict(num_free=99), dict(num_free=1 << 31), dict(num_pages=1), dict(num_pages=1 << 31, num_free=1 << 31), dict(most=0),
@@ -183,7 +183,7 @@ def test_pages_compact_refusals():
         assert call(**bad) == ERR_SHAPE, bad
     for name in ins + outs:
         assert call(**{name: A * 50 + 2}) == ERR_ALIGN, name
-    assert call(ws=None) == ERR_WORKSPACE and call(nb=431) == ERR_WORKSPACE and call(ws=40 * A + 8) == ERR_ALIGN
+    assert call(ws=None) == ERR_WORKSPACE and call(nb=415) == ERR_WORKSPACE and call(ws=40 * A + 8) == ERR_ALIGN
 
 
 def test_the_binding_refuses_before_the_library():
