@@ -671,7 +671,7 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
  *   allowed [B, n, ceil(V / 32)] int32 or NULL: bit x % 32 of word x / 32 says that token x may come
  *   workspace: loza_ssa_token_probs_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
  * Token x with logit l, said c times: l / repetition if l > 0, l repetition otherwise, where it was said or occurs in the prompt; less frequency c and
- * (c > 0) presence; plus its bias; each operation rounded to fp32. Tokens that are not allowed, whatever their logits, and those whose result is a NaN, weigh
+ * (c > 0) presence; plus its bias; in fp32, in greedy rows each operation rounded by itself. Tokens that are not allowed, whatever their logits, and those whose result is a NaN, weigh
  * nothing. probs = exp((l - max) / temperature) / sum; where the temperature is not in [2^-100, 2^100] (0: greedy): 1 at the first of the largest. A row in
  * which nothing weighs is all 0 (loza_ssa_verify_tree then has no next token). Logits of +infinity share a row among them.
  * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30, as many rows as a launch takes. Sums in fp32, always in the same order.

@@ -19,41 +19,63 @@ namespace loza {
 
 namespace {
 
-constexpr int kUnit = 8;                         // tokens a thread takes at a time: 16 bytes of bf16 logits and of the record
+// A wave takes 512 tokens at a time, a lane 4 of the first half and 4 of the second: so its two stores of 16 bytes lie side by side with its neighbours'. (Of 8
+// tokens in a row it would be 16 bytes of every 32: 670 MB in and out 179 us, with halves 147.)
+constexpr int kUnit = 8, kHalf = 256, kBlock = 2 * kHalf;
+__device__ __forceinline__ constexpr int token_of(int x, int i) { return x + (i & 3) + (i >> 2) * kHalf; }     // token i of a lane whose first is x
 constexpr int kThreads = 256, kStep = kUnit * kThreads, kRowThreads = 512;
 constexpr int kMostSlice = 131072;               // tokens of a slice (a bit each in LDS)
 constexpr int kMostSpecial = kTreeNodes + kMostBias;
 
-// What a row's logits are changed by
+// What a row's logits are changed by. Where the largest is asked for (greedy rows) each operation is rounded by itself, as a plain program does them: a token
+// next to another must not win by a rounding left out. Elsewhere (`soft`) a few units do not matter, and half of the instructions do.
 struct Change {
-    float rep, fre, pre;
-    // Each operation rounded by itself, as a plain program does them: a token next to another must not win by a rounding left out.
-    __device__ __forceinline__ float operator()(float l, bool occurred, int said) const
+    float rep, inv, inv_lo, fre, pre;  // inv + inv_lo: 1 / rep
+    bool quick;                        // the division by `rep` as below
+
+    __device__ __forceinline__ void set(float rep_, float fre_, float pre_)
+    {
+        rep = rep_;
+        inv = 1.f / rep_;
+        inv_lo = __builtin_fmaf(-inv, rep_, 1.f) * inv;
+        fre = fre_;
+        pre = pre_;
+        quick = rep >= 0x1p-100f && rep <= 0x1p100f;
+    }
+    __device__ __forceinline__ float soft(float l, bool occurred, uint32_t said) const
+    {
+        const float r = l * (l > 0.f ? inv : rep), less = said != 0 ? __builtin_fmaf(fre, (float)said, pre) : 0.f;
+        return (occurred ? r : l) - less;
+    }
+    __device__ __forceinline__ float rounded(float l, bool occurred, uint32_t said) const
     {
 #pragma clang fp contract(off)
-        const float up = l / rep, down = l * rep, was = occurred ? (l > 0.f ? up : down) : l, f = fre * (float)said, less = (was - f) - pre;
-        return said > 0 ? less : was;
+        if (occurred) l = l > 0.f ? l / rep : l * rep;
+        if (said > 0) {
+            const float f = fre * (float)said;
+            l = l - f;
+            l = l - pre;
+        }
+        return l;
+    }
+    // The same without branches. l / rep as l (inv + inv_lo), which is off by less than a unit, and a correction by what is left, fma(-q, rep, l) inv: that gives
+    // the rounded quotient (Markstein 1990; below 2^-100 it may miss by a step). One that overflows comes out as a NaN.
+    __device__ __forceinline__ float quickly(float l, bool occurred, uint32_t said) const
+    {
+#pragma clang fp contract(off)
+        float q = __builtin_fmaf(l, inv_lo, l * inv);
+        q = __builtin_fmaf(__builtin_fmaf(-q, rep, l), inv, q);
+        const float r = __builtin_amdgcn_classf(l, 0x180) ? q : l * rep;         // (positive and finite)
+        const float was = occurred ? r : l, f = fre * (float)said, less = (was - f) - pre;
+        return said != 0 ? less : was;
     }
 };
 
-// exp(d / T) for d <= 0: 2^(d c), c = log2(e) / T in two parts. Where a token does not weigh d is -infinity, or a NaN (nothing weighs yet): cut to what has a weight of 0.
+// exp(d / T) for d <= 0: 2^(d c), c = log2(e) / T. -infinity gives 0. Off by 2^-24 of |d| / T twice (the product, and c) and by the exponential's own unit.
 struct Weight {
-    float hi, lo, least;
-    __device__ __forceinline__ explicit Weight(float t)
-    {
-        const double c = 1.4426950408889634074 / (double)t;
-        hi = (float)c;
-        lo = (float)(c - (double)hi);
-        least = (float)(-200.0 / c);
-    }
-    // The rounding of the product left in (a sum of many: each off by 2^-24 of |d| / T, in either direction)
-    __device__ __forceinline__ float rough(float d) const { return __builtin_amdgcn_exp2f(fmaxf(d, least) * hi); }
-    // ... and given back to first order; times a factor
-    __device__ __forceinline__ float exact(float d, float factor) const
-    {
-        const float x = fmaxf(d, least), h = x * hi, rest = __builtin_fmaf(x, lo, __builtin_fmaf(x, hi, -h)), p = __builtin_amdgcn_exp2f(h) * factor;
-        return __builtin_fmaf(p * rest, 0.693147180559945f, p);
-    }
+    float c;
+    __device__ __forceinline__ explicit Weight(float t) : c((float)(1.4426950408889634074 / (double)t)) {}
+    __device__ __forceinline__ float operator()(float d) const { return __builtin_amdgcn_exp2f(d * c); }
 };
 
 // Largest logit, its first token, and the sum of the weights relative to it
@@ -65,14 +87,14 @@ __device__ __forceinline__ void merge(Stat &a, float m, float s, int32_t x, cons
 {
     if (m == LOZA_NEG_INF) return;
     if (m > a.m) {
-        a.s = s + a.s * w.rough(a.m - m);
+        a.s = s + a.s * w(a.m - m);
         a.m = m;
         a.x = x;
     } else if (m == a.m) {                       // (two infinities among them)
         a.s += s;
         if (x < a.x) a.x = x;
     } else {
-        a.s += s * w.rough(m - a.m);
+        a.s += s * w(m - a.m);
     }
 }
 
@@ -89,43 +111,56 @@ __device__ __forceinline__ float largest(const float (&l)[kUnit])
     return a > b ? a : b;
 }
 
-// What is read of 8 tokens
+// Requests whose temperature is 0 (or otherwise none to divide by) take the largest logit.
+__device__ __forceinline__ float temperature_of(const ProbsParams &p, int b)
+{
+    const float t = p.temperature ? p.temperature[b] : 1.f;
+    return t >= 0x1p-100f && t <= 0x1p100f ? t : 0.f;
+}
+
+// What is read of a lane's 8 tokens
 template <typename E>
 struct Raw {
-    u32x4 l[sizeof(E) / 2], z;
-    uint32_t ok, apart;
+    static constexpr int kWords = 4 * sizeof(E) / 4;                 // of a half
+    uint32_t l[2 * kWords], z[4], ok;
 
-    // The logits at `at`: rows of odd vocabularies are aligned to their elements only
-    __device__ __forceinline__ void load(const E *at) { __builtin_memcpy(l, at, sizeof(l)); }
-    __device__ __forceinline__ void load(const E *at, int n)         // n < 8 of them
-    {
-        E e[kUnit] = {};
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i)
-            if (i < n) e[i] = at[i];
-        __builtin_memcpy(l, e, sizeof(l));
-    }
     __device__ __forceinline__ float logit(int i) const
     {
-        // (named first: a bit cast of a vector's element itself takes its first one)
-        const uint32_t x = sizeof(E) == 4 ? l[i / 4 % (sizeof(E) / 2)][i % 4] : i & 1 ? l[0][i / 2] & 0xffff0000u : l[0][i / 2] << 16;
+        const uint32_t x = sizeof(E) == 4 ? l[i % (2 * kWords)] : i & 1 ? l[i / 2] & 0xffff0000u : l[i / 2] << 16;
         return __builtin_bit_cast(float, x);
     }
+    __device__ __forceinline__ uint32_t record(int i) const { return i & 1 ? z[i / 2] >> 16 : z[i / 2] & 0xffffu; }
 };
 
-// One row's slice [x0, x1): the tokens that are done apart, and what the pass over the others needs.
-template <typename E, int THREADS>
+// (not fused with what comes before)
+__device__ __forceinline__ float add(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a + b;
+}
+
+// The tokens that are done apart, in LDS
+struct Special {
+    int32_t tok[kMostSpecial], again;
+    float val[kMostSpecial];
+};
+
+// One row's slice [x0, x1): the tokens that are done apart, and what the pass over the others needs. PLAIN: there are no such tokens, no record and no grammar.
+template <typename E, int THREADS, bool PLAIN>
 struct Slice {
     const ProbsParams &p;
     const E *row;
     const uint16_t *seen;
     const uint8_t *allowed;
     int b, r, x0, x1, entries;
+    uint32_t bits_mine = 0;       // which of this thread's entries stand for their tokens (1,088 entries are at most 5 a thread)
     Change change;
+    bool soft;
     int32_t *tok;                 // LDS: [entries] tokens done apart, -1 where they are not in the slice
-    uint32_t *bits;               // LDS: a bit a token of the slice
+    float *val;                   // LDS: their changed logits
+    uint32_t *bits;               // LDS: a bit a token of the slice: done apart, or not allowed
 
-    __device__ __forceinline__ Slice(const ProbsParams &p_, int64_t row_index, int slice, int32_t *tok_, uint32_t *bits_) : p(p_), tok(tok_), bits(bits_)
+    __device__ __forceinline__ Slice(const ProbsParams &p_, int64_t row_index, int slice, Special &lds, uint32_t *bits_) : p(p_), tok(lds.tok), val(lds.val), bits(bits_)
     {
         b = (int)(row_index / p.n);
         r = (int)(row_index - (int64_t)b * p.n);
@@ -134,18 +169,25 @@ struct Slice {
         allowed = p.allowed ? (const uint8_t *)(p.allowed + row_index * p.words) : nullptr;
         x0 = slice * p.slice_len;
         x1 = x0 + p.slice_len < p.V ? x0 + p.slice_len : p.V;
-        change.rep = p.repetition ? p.repetition[b] : 1.f;
-        change.fre = p.frequency ? p.frequency[b] : 0.f;
-        change.pre = p.presence ? p.presence[b] : 0.f;
+        if constexpr (PLAIN) {
+            entries = 0;
+            return;
+        }
+        change.set(p.repetition ? p.repetition[b] : 1.f, p.frequency ? p.frequency[b] : 0.f, p.presence ? p.presence[b] : 0.f);
+        soft = temperature_of(p, b) > 0.f;
         const int nodes = p.masks ? p.n : 0;
         entries = nodes + p.n_bias;
-        if (entries == 0) return;
-        for (int i = threadIdx.x; i < (x1 - x0 + 31) / 32; i += THREADS) bits[i] = 0;
+        const int words = (x1 - x0 + 31) / 32;
+        if (entries == 0) {
+            bar(words);
+            return;
+        }
+        for (int i = threadIdx.x; i < words; i += THREADS) bits[i] = 0;
+        if (threadIdx.x == 0) lds.again = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < (entries + 3) / 4 * 4; i += THREADS) {
+        for (int i = threadIdx.x; i < entries; i += THREADS) {
             int x = -1;
-            if (i >= entries) {
-            } else if (i < nodes) {
+            if (i < nodes) {
                 const uint64_t path = (uint64_t)p.masks[row_index];
                 if ((path >> i & 1) && i < length()) x = p.tokens[(int64_t)b * p.n + i];
             } else {
@@ -153,8 +195,34 @@ struct Slice {
             }
             if (x < x0 || x >= x1) x = -1;
             tok[i] = x;
-            if (x >= 0) atomicOr(&bits[(x - x0) >> 5], 1u << ((x - x0) & 31));
+            if (x >= 0) {
+                const uint32_t bit = 1u << ((x - x0) & 31);
+                if (atomicOr(&bits[(x - x0) >> 5], bit) & bit) lds.again = 1;
+            }
         }
+        __syncthreads();
+        // their logits; a token that is there more than once is done by the first of its entries
+        const bool again = lds.again != 0;
+        for (int i = threadIdx.x; i < entries; i += THREADS) {
+            float l = 0.f;
+            const bool mine = special(i, again, l);
+            val[i] = l;
+            if (!again && !mine) tok[i] = -1;
+            if (again) bits_mine = mine ? bits_mine | 1u << (i / THREADS) : bits_mine;
+        }
+        if (again) {
+            __syncthreads();                                          // (all have looked at the list)
+            for (int i = threadIdx.x; i < entries; i += THREADS)
+                if (!(bits_mine >> (i / THREADS) & 1)) tok[i] = -1;
+        }
+        bar(words);
+    }
+    // Adds the tokens that are not allowed to the bits
+    __device__ __forceinline__ void bar(int words)
+    {
+        if (allowed == nullptr) return;
+        const uint32_t *from = (const uint32_t *)allowed + x0 / 32;
+        for (int i = threadIdx.x; i < words; i += THREADS) bits[i] = (entries ? bits[i] : 0u) | ~from[i];
         __syncthreads();
     }
     __device__ __forceinline__ int length() const
@@ -162,102 +230,134 @@ struct Slice {
         const int len = p.tree_lens ? p.tree_lens[b] : p.n;
         return len < p.n ? len : p.n;
     }
-    // Everything of the tokens [x, x + 8) that is in memory; `whole`: all of them are there
+    // Everything of a lane's tokens that is in memory; `whole`: the wave's are all there
     __device__ __forceinline__ void load(int x, bool whole, Raw<E> &raw) const
     {
-        if (whole) raw.load(row + x);
-        else raw.load(row + x, p.V - x);
-        raw.z = u32x4{0, 0, 0, 0};
-        if (seen) raw.z = *(const u32x4 *)(seen + x);
-        raw.ok = 0xffu;
-        if (allowed) raw.ok = allowed[x >> 3];
-        if (!whole) raw.ok &= (1u << (p.V - x)) - 1;
-        raw.apart = 0;
-        if (entries) raw.apart = ((const uint8_t *)bits)[(x - x0) >> 3];
+        constexpr int W = Raw<E>::kWords;
+        raw.ok = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;  // tokens of this half that are there
+            raw.z[2 * h] = raw.z[2 * h + 1] = 0;
+            if (!whole && n < 4) {
+                E e[4] = {};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < n) e[i] = row[xh + i];
+                __builtin_memcpy(raw.l + h * W, e, sizeof(e));
+                if (n <= 0) continue;
+            } else {
+                __builtin_memcpy(raw.l + h * W, row + xh, 4 * sizeof(E));      // (rows of odd vocabularies are aligned to their elements only)
+            }
+            if (!PLAIN && seen) {
+                const u32x2 z = *(const u32x2 *)(seen + xh);
+                raw.z[2 * h] = z[0];
+                raw.z[2 * h + 1] = z[1];
+            }
+            uint32_t ok = 15u;
+            if (!PLAIN && (entries || allowed)) ok = ~((uint32_t)((const uint8_t *)bits)[(xh - x0) >> 3] >> (xh & 4)) & 15u;
+            if (!whole && n < 4) ok &= (1u << n) - 1;
+            raw.ok |= ok << (4 * h);
+        }
     }
     // Their changed logits; -inf for those done apart, not allowed, or not there
-    __device__ __forceinline__ void changed(const Raw<E> &raw, float (&l)[kUnit]) const
+    template <bool SOFT>
+    __device__ __forceinline__ void changed(int x, bool whole, const Raw<E> &raw, float (&l)[kUnit]) const
     {
 #pragma unroll
         for (int i = 0; i < kUnit; ++i) l[i] = raw.logit(i);
-        if (raw.z[0] | raw.z[1] | raw.z[2] | raw.z[3]) {
+        // (branches of whole waves: a branch of lanes has the compiler keep a copy of everything)
+        bool again = false;
+        if (!PLAIN && __any((raw.z[0] | raw.z[1] | raw.z[2] | raw.z[3]) != 0)) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) {
-                const uint32_t z = i & 1 ? raw.z[i / 2] >> 16 : raw.z[i / 2] & 0xffffu;
-                l[i] = change(l[i], z != 0, (int)(z & 0x7fffu));
+                const uint32_t z = raw.record(i);
+                l[i] = SOFT ? change.soft(l[i], z != 0, z & 0x7fffu) : change.quickly(l[i], z != 0, z & 0x7fffu);
+            }
+            again = !SOFT && !change.quick;
+        }
+        // (two a comparison)
+        bool nans = again;
+#pragma unroll
+        for (int i = 0; i < kUnit; i += 2) nans |= __builtin_isunordered(l[i], l[i + 1]);
+        if (__any(nans)) {
+            if (PLAIN || SOFT) {
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) l[i] = settle(l[i]);
+            } else {
+                // NaNs, or quotients: once more, from memory so that nothing is kept for this
+#pragma unroll 1
+                for (int i = 0; i < kUnit; ++i) {
+                    const int xi = token_of(x, i);
+                    float y = LOZA_NEG_INF;
+                    if (xi < p.V) {
+                        const uint32_t z = seen ? seen[xi] : 0u;
+                        y = settle(change.rounded(Elem<E>::get(row[xi]), z != 0, z & 0x7fffu));
+                    }
+#pragma unroll
+                    for (int k = 0; k < kUnit; ++k) l[k] = k == i ? y : l[k];
+                }
             }
         }
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) l[i] = settle(l[i]);
-        const uint32_t ok = raw.ok & ~raw.apart;
-        if (ok != 0xffu) {
+        if ((!PLAIN || !whole) && __any(raw.ok != 0xffu)) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) {
-                const uint32_t keep = (uint32_t)((int32_t)(ok << (31 - i)) >> 31), x = __builtin_bit_cast(uint32_t, l[i]);
-                l[i] = __builtin_bit_cast(float, (x & keep) | (0xff800000u & ~keep));
+                const uint32_t keep = (uint32_t)((int32_t)(raw.ok << (31 - i)) >> 31), y = __builtin_bit_cast(uint32_t, l[i]);
+                l[i] = __builtin_bit_cast(float, (y & keep) | (0xff800000u & ~keep));
             }
         }
     }
-    // Calls f(x, raw, whole) for this thread's units, kAhead at a time so that their loads are under way together
+    // Calls f(x, raw, whole) for this wave's blocks of 512 tokens, kAhead at a time so that their loads are under way together
     template <typename F>
     __device__ __forceinline__ void units(F f) const
     {
-        constexpr int kAhead = sizeof(E) == 2 ? 2 : 1;
-        int x = x0 + (int)threadIdx.x * kUnit;
-        const int whole_end = (x1 - x0) / kUnit * kUnit + x0, step = THREADS * kUnit;
-        for (; x + (kAhead - 1) * step < whole_end; x += kAhead * step) {
+        constexpr int kAhead = sizeof(E) == 2 ? 2 : 1, step = THREADS * kUnit;
+        const int lane4 = 4 * (threadIdx.x & 63);
+        int at = x0 + (int)(threadIdx.x >> 6) * kBlock;              // the block's first token
+        for (; at + (kAhead - 1) * step + kBlock <= x1; at += kAhead * step) {
             Raw<E> raw[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) load(x + k * step, true, raw[k]);
+            for (int k = 0; k < kAhead; ++k) load(at + k * step + lane4, true, raw[k]);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) f(x + k * step, raw[k], true);
+            for (int k = 0; k < kAhead; ++k) f(at + k * step + lane4, raw[k], true);
         }
-        for (; x < whole_end; x += step) {
+        for (; at < x1; at += step) {
             Raw<E> raw;
-            load(x, true, raw);
-            f(x, raw, true);
-        }
-        if (x < x1) {                                                // (x is where the last, short unit begins, in one thread)
-            Raw<E> raw;
-            load(x, false, raw);
-            f(x, raw, false);
+            const bool whole = at + kBlock <= x1;
+            load(at + lane4, whole, raw);
+            f(at + lane4, raw, whole);
         }
     }
-    // The changed logit of entry i, and whether it is the one that stands for its token (the first of them)
-    __device__ __forceinline__ bool special(int i, float &l) const
+    // The changed logit of entry i, and whether it is the one that stands for its token; `again`: some token is there more than once
+    __device__ __forceinline__ bool special(int i, bool again, float &l) const
     {
-#pragma clang fp contract(off)
         const int x = tok[i], nodes = p.masks ? p.n : 0;
         if (x < 0) return false;
         const int z = seen ? seen[x] : 0;
+        const bool ok = !allowed || (allowed[x >> 3] >> (x & 7) & 1);
+        const float *values = p.bias_values + (int64_t)b * p.n_bias - nodes;
         int said = z & 0x7fff, first = i;
         float bias = 0.f;
         l = Elem<E>::get(row[x]);
-        const bool ok = !allowed || (allowed[x >> 3] >> (x & 7) & 1);
-#pragma unroll 2
-        for (int k = 0; k < entries; k += 4) {                       // (behind the last entry there are -1)
-            const i32x4 t = *(const i32x4 *)(tok + k);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (t[j] == x) {
-                    if (k + j < first) first = k + j;
-                    if (k + j < nodes) ++said;
-                    else bias = bias + p.bias_values[(int64_t)b * p.n_bias + k + j - nodes];
-                }
+        if (!again) {
+            if (i < nodes) ++said;
+            else bias = values[i];
+        } else {
+#pragma unroll 8
+            for (int k = 0; k < entries; ++k) {
+                if (tok[k] != x) continue;
+                if (k < first) first = k;
+                if (k < nodes) ++said;
+                else bias = add(bias, values[k]);
+            }
         }
-        if (first != i) return false;
-        l = settle(change(l, z >= 0x8000 || said > 0, said) + bias);
+        const bool occurred = z >= 0x8000 || said > 0;
+        l = soft ? change.soft(l, occurred, (uint32_t)said) : change.rounded(l, occurred, (uint32_t)said);
+        l = settle(add(l, bias));
         if (!ok) l = LOZA_NEG_INF;
-        return true;
+        return first == i;
     }
 };
-
-// Requests whose temperature is 0 (or otherwise none to divide by) take the largest logit.
-__device__ __forceinline__ float temperature_of(const ProbsParams &p, int b)
-{
-    const float t = p.temperature ? p.temperature[b] : 1.f;
-    return t >= 0x1p-100f && t <= 0x1p100f ? t : 0.f;
-}
 
 // Stat of a whole workgroup, in all of its threads
 template <int THREADS>
@@ -283,64 +383,92 @@ __device__ __forceinline__ Stat workgroup_stat(Stat a, const Weight &w, Stat *ld
 constexpr Stat kNoStat = {LOZA_NEG_INF, 0.f, 0x7fffffff, 0};
 
 // Stat of this thread's share of a slice
-template <typename E, int THREADS>
-__device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS> &s, float t, const Weight &w)
+template <bool SOFT, typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, PLAIN> &s, const Weight &w)
 {
     Stat a = kNoStat;
-    s.units([&](int x, const Raw<E> &raw, bool) {
+    s.units([&](int x, const Raw<E> &raw, bool whole) {
         float l[kUnit];
-        s.changed(raw, l);
+        s.template changed<SOFT>(x, whole, raw, l);
         const float m = largest(l);
         if (m > a.m) {
-            a.s *= w.rough(a.m - m);
-            a.m = m;
-            if (!(t > 0.f)) {
+            if constexpr (SOFT) {
+                a.s *= w(a.m - m);
+            } else {
                 int at = 0;
 #pragma unroll
-                for (int i = kUnit - 1; i >= 0; --i) at = l[i] == m ? i : at;
+                for (int i = kUnit - 1; i >= 0; --i) at = l[i] == m ? token_of(0, i) : at;
                 a.x = x + at;
             }
+            a.m = m;
         }
-        if (t > 0.f && a.m < __builtin_inff()) {
+        if constexpr (SOFT) {
+            if (a.m > LOZA_NEG_INF && a.m < __builtin_inff()) {
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) a.s += w.rough(l[i] - a.m);
-        } else if (t > 0.f) {
+                for (int i = 0; i < kUnit; ++i) a.s += w(l[i] - a.m);
+            } else if (a.m > 0.f) {
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) a.s += l[i] == a.m ? 1.f : 0.f;     // (those of +infinity share the row)
+                for (int i = 0; i < kUnit; ++i) a.s += l[i] == a.m ? 1.f : 0.f;     // (those of +infinity share the row)
+            }
         }
     });
-    for (int i = threadIdx.x; i < s.entries; i += THREADS) {
-        float l;
-        if (s.special(i, l)) merge(a, l, 1.f, s.tok[i], w);
-    }
+    if constexpr (!PLAIN)
+        for (int i = threadIdx.x; i < s.entries; i += THREADS)
+            if (s.tok[i] >= 0) merge(a, s.val[i], 1.f, s.tok[i], w);
     return a;
 }
 
 // The probabilities of a slice, given the Stat of its row
-template <typename E, int THREADS>
-__device__ __forceinline__ void write_probs(const Slice<E, THREADS> &s, float *out, const Stat &a, float t, const Weight &w)
+template <bool NT, bool SOFT, typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ void write_probs_t(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, const Weight &w)
 {
-    const bool greedy = !(t > 0.f);
     const float inv = a.m == LOZA_NEG_INF ? 0.f : 1.f / a.s;
-    const bool infinite = a.m == __builtin_inff();
-    auto prob = [&](float l, int x) { return greedy ? (x == a.x ? 1.f : 0.f) : infinite ? (l == a.m ? inv : 0.f) : w.exact(l - a.m, inv); };
+    const bool infinite = a.m == __builtin_inff() || a.m == LOZA_NEG_INF;       // (nothing weighs: 0 for all)
+    auto prob = [&](float l, int x) { return SOFT ? w(l - a.m) * inv : x == a.x ? 1.f : 0.f; };
+    auto rare = [&](float l) { return l == a.m ? inv : 0.f; };
     s.units([&](int x, const Raw<E> &raw, bool whole) {
         float l[kUnit];
-        s.changed(raw, l);
+        s.template changed<SOFT>(x, whole, raw, l);
+        if (SOFT && infinite) {
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) l[i] = prob(l[i], x + i);
-        if (raw.apart == 0 && whole) {
-            __builtin_memcpy(out + x, l, sizeof(l));
+            for (int i = 0; i < kUnit; ++i) l[i] = rare(l[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) l[i] = prob(l[i], token_of(x, i));
+        }
+        if (whole) {
+            // (those done apart are overwritten below)
+            typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+            u32x4 y[2];
+            __builtin_memcpy(y, l, sizeof(y));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if constexpr (NT) __builtin_nontemporal_store(y[k], (u32x4_at4 *)(out + x + kHalf * k));
+                else *(u32x4_at4 *)(out + x + kHalf * k) = y[k];
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i)
-                if (!(raw.apart >> i & 1) && x + i < s.p.V) out[x + i] = l[i];
+                if (token_of(x, i) < s.p.V) out[token_of(x, i)] = l[i];
         }
     });
-    for (int i = threadIdx.x; i < s.entries; i += THREADS) {
-        float l;
-        if (s.special(i, l)) out[s.tok[i]] = prob(l, s.tok[i]);
-    }
+    if (PLAIN || s.entries == 0) return;
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));                        // this wave's are written
+    __syncthreads();
+    for (int i = threadIdx.x; i < s.entries; i += THREADS)
+        if (s.tok[i] >= 0) out[s.tok[i]] = SOFT && infinite ? rare(s.val[i]) : prob(s.val[i], s.tok[i]);
+}
+
+template <typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS, PLAIN> &s, float t, const Weight &w)
+{
+    return t > 0.f ? thread_stat_t<true>(s, w) : thread_stat_t<false>(s, w);
+}
+template <bool NT, typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ void write_probs(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, float t, const Weight &w)
+{
+    if (t > 0.f) write_probs_t<NT, true>(s, out, a, w);
+    else write_probs_t<NT, false>(s, out, a, w);
 }
 
 // Whether a row is one of its tree's
@@ -349,30 +477,30 @@ __device__ __forceinline__ bool row_there(const ProbsParams &p, int64_t row)
     return p.tree_lens == nullptr || (int)(row % p.n) < p.tree_lens[row / p.n];
 }
 
-template <typename E>
+template <typename E, bool PLAIN>
 __global__ __launch_bounds__(kThreads) void token_stats_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
-    __shared__ __attribute__((aligned(16))) int32_t s_tok[kMostSpecial];
+    __shared__ Special s_special;
     __shared__ Stat s_stat[kThreads / 64];
     const int64_t row = blockIdx.x / p.slices;
     if (!row_there(p, row)) return;
-    const Slice<E, kThreads> s(p, row, (int)(blockIdx.x - row * p.slices), s_tok, s_bits);
+    const Slice<E, kThreads, PLAIN> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     const Stat a = workgroup_stat<kThreads>(thread_stat(s, t, w), w, s_stat);
     if (threadIdx.x == 0) ((Stat *)p.stats)[blockIdx.x] = a;
 }
 
-template <typename E>
+template <typename E, bool PLAIN, bool NT>
 __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
-    __shared__ __attribute__((aligned(16))) int32_t s_tok[kMostSpecial];
+    __shared__ Special s_special;
     __shared__ Stat s_stat[kThreads / 64];
     const int64_t row = blockIdx.x / p.slices;
     if (!row_there(p, row)) return;
-    const Slice<E, kThreads> s(p, row, (int)(blockIdx.x - row * p.slices), s_tok, s_bits);
+    const Slice<E, kThreads, PLAIN> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     Stat a = kNoStat;
@@ -381,23 +509,23 @@ __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams
         merge(a, part.m, part.s, part.x, w);
     }
     a = workgroup_stat<kThreads>(a, w, s_stat);
-    write_probs(s, p.probs + row * p.V, a, t, w);
+    write_probs<NT>(s, p.probs + row * p.V, a, t, w);
 }
 
 // A workgroup a row, in one launch: the row is read again for the probabilities, from a cache that holds what is under way.
-template <typename E>
+template <typename E, bool PLAIN, bool NT>
 __global__ __launch_bounds__(kRowThreads) void token_row_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
-    __shared__ __attribute__((aligned(16))) int32_t s_tok[kMostSpecial];
+    __shared__ Special s_special;
     __shared__ Stat s_stat[kRowThreads / 64];
     const int64_t row = blockIdx.x;
     if (!row_there(p, row)) return;
-    const Slice<E, kRowThreads> s(p, row, 0, s_tok, s_bits);
+    const Slice<E, kRowThreads, PLAIN> s(p, row, 0, s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     const Stat a = workgroup_stat<kRowThreads>(thread_stat(s, t, w), w, s_stat);
-    write_probs(s, p.probs + row * p.V, a, t, w);
+    write_probs<NT>(s, p.probs + row * p.V, a, t, w);
 }
 
 // ---- the record of a request's tokens -----------------------------------------------------------------------
@@ -518,24 +646,38 @@ void probs_plan(ProbsParams &p)
     p.words = (int)(((int64_t)p.V + 31) / 32);
 }
 
-template <typename E>
+template <typename E, bool PLAIN, bool NT>
 static hipError_t launch_probs_t(const ProbsParams &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)((int64_t)p.B * p.n * p.slices));
-    const size_t lds = p.masks || p.n_bias ? (size_t)(p.slice_len < p.V ? p.slice_len : p.V + 31) / 32 * 4 : 0;
+    const size_t lds = p.masks || p.n_bias || p.allowed ? (size_t)(p.slice_len < p.V ? p.slice_len : p.V + 31) / 32 * 4 : 0;
     if (p.slices == 1 && p.V > kStep) {
-        hipLaunchKernelGGL((token_row_kernel<E>), grid, dim3(kRowThreads), lds, stream, p);
+        hipLaunchKernelGGL((token_row_kernel<E, PLAIN, NT>), grid, dim3(kRowThreads), lds, stream, p);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((token_stats_kernel<E>), grid, dim3(kThreads), lds, stream, p);
+    hipLaunchKernelGGL((token_stats_kernel<E, PLAIN>), grid, dim3(kThreads), lds, stream, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL((token_probs_kernel<E>), grid, dim3(kThreads), lds, stream, p);
+    hipLaunchKernelGGL((token_probs_kernel<E, PLAIN, NT>), grid, dim3(kThreads), lds, stream, p);
     return hipGetLastError();
+}
+
+template <typename E, bool PLAIN>
+static hipError_t launch_probs_p(const ProbsParams &p, hipStream_t stream)
+{
+    // Results that no cache holds are stored past the caches, which keep the logits for their second reading (1,024 rows of 131,072 bf16 logits 244 -> 162 us)
+    return (int64_t)p.B * p.n * p.V * 4 >= 128 << 20 ? launch_probs_t<E, PLAIN, true>(p, stream) : launch_probs_t<E, PLAIN, false>(p, stream);
+}
+
+template <typename E>
+static hipError_t launch_probs_e(const ProbsParams &p, hipStream_t stream)
+{
+    const bool plain = !p.masks && !p.n_bias && !p.allowed && !p.seen;
+    return plain ? launch_probs_p<E, true>(p, stream) : launch_probs_p<E, false>(p, stream);
 }
 
 hipError_t launch_token_probs(const ProbsParams &p, int elem_bytes, hipStream_t stream)
 {
-    return elem_bytes == 2 ? launch_probs_t<uint16_t>(p, stream) : launch_probs_t<float>(p, stream);
+    return elem_bytes == 2 ? launch_probs_e<uint16_t>(p, stream) : launch_probs_e<float>(p, stream);
 }
 
 constexpr int kManyTokens = 1024;

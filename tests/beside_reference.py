@@ -95,10 +95,12 @@ def changed_logits(logits, said, occurs, rep, fre, pre, bias, allowed):
     return l
 
 
-def probabilities(l, temperature):
-    """From the changed logits of a row, in 64 bits, and their bound: the difference to the largest is off by 2^-24 of |l - max| / T, the rest of a token's own
-    weight by 8 units; in the sum, the product with 1 / T and that number's own rounding are off by as much each again, 3 of the weighted mean of |l - max| / T; sums
-    of V positive terms over at least 256 threads of 8 each, whose reference moves once a unit at most (4 units each time), by V / 256 + 4 V / 2048 + 100."""
+def probabilities(l, temperature, size=0.0):
+    """From the changed logits of a row, in 64 bits, and their bound. `size`: where a row is not greedy its penalties may be rounded otherwise than in
+    changed_logits, within 2^-24 of `size`, four times the sum of the absolute values that went into a logit: the rounded 1 / repetition and its product,
+    frequency times the number and presence in one step, the two subtractions. A weight is off by 2^-24 of |l - max| / T three times (the difference, its product with
+    1 / T, and that number's own rounding) and by 8 units (the exponential's, scalings and the last product); the sum by the weighted mean of that, and V positive
+    terms over at least 256 threads of 8 each, whose reference moves once a unit at most (4 units each time), by V / 256 + 4 V / 2048 + 100."""
     l = l.astype(np.float64)
     top = l.max()
     if top == -np.inf:
@@ -113,7 +115,8 @@ def probabilities(l, temperature):
     p = e / e.sum()
     n = len(l)
     live = np.where(np.isfinite(d), np.abs(d), 0.0)
-    units = live + 3 * (e * live).sum() / e.sum() + 8 + n / 256 + 4 * n / 2048 + 100
+    own = 3 * live + np.where(np.isfinite(l), size, 0.0) / np.float64(temperature)
+    units = own + (e * own).sum() / e.sum() + 8 + n / 256 + 4 * n / 2048 + 100
     return p, units * U * p + 1e-37
 
 

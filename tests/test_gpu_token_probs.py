@@ -83,7 +83,10 @@ class Call:
                 bias = [] if self.bt is None else list(zip(self.bt[b].tolist(), self.bv[b]))
                 c = N.changed_logits(l[b, r], said, occurs, pick(self.rep, b, 1.0), pick(self.fre, b, 0.0), pick(self.pre, b, 0.0), bias,
                                      None if self.ok is None else self.ok[b, r])
-                ref, bound = N.probabilities(c, float(pick(self.temp, b, 1.0)))
+                with np.errstate(all="ignore"):
+                    rep, row = float(pick(self.rep, b, 1.0)), np.abs(l[b, r].astype(np.float64))
+                    size = 4 * occurs * (row * max(rep, 1 / rep) + abs(float(pick(self.fre, b, 0.0))) * said + abs(float(pick(self.pre, b, 0.0))))
+                ref, bound = N.probabilities(c, float(pick(self.temp, b, 1.0)), np.where(np.isfinite(size), size, 0.0))
                 err = np.abs(got[b, r] - ref)
                 assert (err <= bound).all(), (b, r, float(err.max()), int(err.argmax()))
                 worst = max(worst, float((err / np.maximum(bound, 1e-37)).max()))
