@@ -74,17 +74,25 @@ struct Lane {
         }
     }
     template <typename E>
-    __device__ __forceinline__ void load(const E *x, float (&v)[NI][2][VEC]) const
+    __device__ __forceinline__ void load(const E *x, Pack<E, VEC> (&raw)[NI][2]) const
     {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                Pack<E, VEC> p{};
-                if (c[j][u] >= 0) p = *(const Pack<E, VEC> *)(x + c[j][u]);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[j][u][e] = Elem<E>::get(p.e[e]);
+                raw[j][u] = {};
+                if (c[j][u] >= 0) raw[j][u] = *(const Pack<E, VEC> *)(x + c[j][u]);
             }
+    }
+    template <typename E>
+    __device__ __forceinline__ static void widen(const Pack<E, VEC> (&raw)[NI][2], float (&v)[NI][2][VEC])
+    {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[j][u][e] = Elem<E>::get(raw[j][u].e[e]);
     }
     template <bool NT, typename E>
     __device__ __forceinline__ void keep(E *out, const float (&v)[NI][2][VEC]) const
@@ -156,83 +164,141 @@ __device__ __forceinline__ void form_angles(const NormParams &p, float2 *sc, int
     }
 }
 
-// Workgroups below q_groups take the queries of `tokens` tokens each, those from there on keys (and values).
+// The heads that a group of lanes takes: of each chunk of `tokens` tokens that its workgroup takes (every `step`-th) the heads g, g + groups, .. of all of them
+struct Rows {
+    int64_t T, step, t0;          // t0: first token of the chunk (T and beyond: none is left)
+    int tokens, H, groups, g, t, h;
+
+    __device__ __forceinline__ Rows(int64_t T_, int64_t first, int64_t step_, int tokens_, int H_, int groups_, int g_)
+        : T(T_), step(step_), t0(first), tokens(tokens_), H(H_), groups(groups_), g(g_), t(0), h(g_)
+    {
+        settle();
+    }
+    __device__ __forceinline__ void settle()
+    {
+        for (; h >= H; h -= H) ++t;
+        if (t >= tokens || t0 + t >= T) t0 = T;                      // (a group that finds none in a chunk finds none in later ones)
+    }
+    __device__ __forceinline__ bool any() const { return t0 < T; }
+    __device__ __forceinline__ int64_t token() const { return t0 + t; }
+    __device__ __forceinline__ void next()
+    {
+        h += groups;
+        for (; h >= H; h -= H) ++t;
+        if (t >= tokens || t0 + t >= T) {
+            t0 += step;
+            t = 0;
+            h = g;
+            settle();
+        }
+    }
+};
+
+// Workgroups below q_groups take the queries, those from there on keys (and values). A group asks for its next head before it works on the one it has: the angles of
+// a chunk, two tables in turn, are formed while heads are on their way.
 template <typename E, int VEC, bool PAIRS, int NI, bool NT>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const NormParams p, const int tokens, const int q_groups)
 {
-    extern __shared__ __attribute__((aligned(16))) float2 sc[];      // [tokens][rot / 2]
+    extern __shared__ __attribute__((aligned(16))) float2 sc[];      // [2][tokens][rot / 2]
     const bool keys = (int)blockIdx.x >= q_groups;
     const NormHeads &n = keys ? p.k : p.q;
-    const int lanes = n.lanes, groups = 256 / lanes, half = p.rot / 2;
-    const int64_t t0 = (int64_t)(blockIdx.x - (keys ? q_groups : 0)) * tokens;
-    const int here = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+    const int lanes = n.lanes, half = p.rot / 2;
+    const int64_t first = (int64_t)(blockIdx.x - (keys ? q_groups : 0)) * tokens, step = (int64_t)(keys ? gridDim.x - q_groups : q_groups) * tokens;
     const Lane<VEC, PAIRS, NI> lane(n, p.rot, p.interleaved, threadIdx.x & (lanes - 1), lanes);
-    form_angles(p, sc, t0, here);
-    __syncthreads();
-    int t = 0, h = threadIdx.x / lanes;
-    for (;; h += groups) {
-        for (; h >= n.r.H; h -= n.r.H) ++t;
-        if (t >= here) break;
-        const int64_t tok = t0 + t;
-        if (p.positions[tok] < 0) continue;                          // padding: nothing is written
-        int64_t to = tok;
-        if (keys) {
-            to = p.slots[tok];
-            if (to < 0 || to >= p.cache_rows) continue;
+    Rows rows(p.T, first, step, tokens, n.r.H, 256 / lanes, threadIdx.x / lanes);
+    Pack<E, VEC> raw[NI][2];
+    int position = -1;
+    auto ask = [&]() {
+        if (!rows.any()) return;
+        lane.load((const E *)n.r.x + rows.token() * n.r.x_token + rows.h * n.r.x_head, raw);
+        position = p.positions[rows.token()];
+    };
+    ask();
+    int turn = 0;
+    for (int64_t t0 = first; t0 < p.T; t0 += step, turn ^= 1) {
+        const int here = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+        float2 *table = sc + turn * tokens * half;
+        form_angles(p, table, t0, here);
+        __syncthreads();
+        while (rows.t0 == t0) {
+            float v[NI][2][VEC];
+            lane.widen(raw, v);
+            const int64_t tok = rows.token();
+            const int t = rows.t, h = rows.h;
+            const bool there = position >= 0;
+            rows.next();
+            ask();
+            if (!there) continue;                                    // padding: nothing is written
+            int64_t to = tok;
+            if (keys) {
+                to = p.slots[tok];
+                if (to < 0 || to >= p.cache_rows) continue;
+            }
+            if (n.norm_dim > 0) {
+                const float r = 1.f / sqrtf(lane.dot(v, v, lanes) / (float)n.norm_dim + p.eps);
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if (lane.normed[j][u]) v[j][u][e] = v[j][u][e] * r * lane.w[j][u][e];
+            }
+            lane.rotate(v, table + t * half, p.rot, n.r.rot_begin, 1.f);
+            lane.template keep<NT>((E *)n.r.out + to * n.r.out_token + h * n.r.out_head, v);
         }
-        float v[NI][2][VEC];
-        lane.load((const E *)n.r.x + tok * n.r.x_token + h * n.r.x_head, v);
-        if (n.norm_dim > 0) {
-            const float r = 1.f / sqrtf(lane.dot(v, v, lanes) / (float)n.norm_dim + p.eps);
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if (lane.normed[j][u]) v[j][u][e] = v[j][u][e] * r * lane.w[j][u][e];
-        }
-        lane.rotate(v, sc + t * half, p.rot, n.r.rot_begin, 1.f);
-        lane.template keep<NT>((E *)n.r.out + to * n.r.out_token + h * n.r.out_head, v);
-    }
-    if (!keys || p.v == nullptr) return;
-    using P = Pack<E, VEC>;
-    const int per = p.d_v / VEC;
-    for (int i = 0; i < here; ++i) {
-        const int64_t tok = t0 + i, slot = p.slots[tok];
-        if (p.positions[tok] < 0 || slot < 0 || slot >= p.cache_rows) continue;
-        for (int k = threadIdx.x; k < per * n.r.H; k += 256) {
-            const int vh = k / per, c = (k - vh * per) * VEC;
-            *(P *)((E *)p.v_rows + (slot * n.r.H + vh) * p.d_v + c) = *(const P *)((const E *)p.v + tok * p.v_token + vh * p.v_head + c);
+        if (!keys || p.v == nullptr) continue;
+        using P = Pack<E, VEC>;
+        const int per = p.d_v / VEC;
+        for (int i = 0; i < here; ++i) {
+            const int64_t tok = t0 + i, slot = p.slots[tok];
+            if (p.positions[tok] < 0 || slot < 0 || slot >= p.cache_rows) continue;
+            for (int k = threadIdx.x; k < per * n.r.H; k += 256) {
+                const int vh = k / per, c = (k - vh * per) * VEC;
+                *(P *)((E *)p.v_rows + (slot * n.r.H + vh) * p.d_v + c) = *(const P *)((const E *)p.v + tok * p.v_token + vh * p.v_head + c);
+            }
         }
     }
 }
 
-// Each workgroup takes `tokens` tokens at a time, as many times as there are, and leaves one partial sum of dw a column.
+// Each workgroup leaves one partial sum of dw a column.
 template <typename E, int VEC, bool PAIRS, int NI, bool NT>
 __global__ __launch_bounds__(256) void norm_rope_backward_kernel(const NormParams p, const int tokens)
 {
-    extern __shared__ __attribute__((aligned(16))) float2 sc[];      // [tokens][rot / 2]
+    extern __shared__ __attribute__((aligned(16))) float2 sc[];      // [2][tokens][rot / 2]
     __shared__ float s_dw[256 * NI * 2 * VEC];
     const NormHeads &n = p.q;
     const int lanes = n.lanes, groups = 256 / lanes, half = p.rot / 2;
+    const int64_t first = (int64_t)blockIdx.x * tokens, step = (int64_t)gridDim.x * tokens;
     const Lane<VEC, PAIRS, NI> lane(n, p.rot, p.interleaved, threadIdx.x & (lanes - 1), lanes);
     float dw[NI][2][VEC] = {};
-    for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < p.T; t0 += (int64_t)gridDim.x * tokens) {
+    Rows rows(p.T, first, step, tokens, n.r.H, groups, threadIdx.x / lanes);
+    Pack<E, VEC> raw_g[NI][2], raw_x[NI][2];
+    int position = -1;
+    auto ask = [&]() {
+        if (!rows.any()) return;
+        lane.load((const E *)p.dout + rows.token() * p.dout_token + rows.h * p.dout_head, raw_g);
+        lane.load((const E *)n.r.x + rows.token() * n.r.x_token + rows.h * n.r.x_head, raw_x);
+        position = p.positions[rows.token()];
+    };
+    ask();
+    int turn = 0;
+    for (int64_t t0 = first; t0 < p.T; t0 += step, turn ^= 1) {
         const int here = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+        float2 *table = sc + turn * tokens * half;
+        form_angles(p, table, t0, here);
         __syncthreads();
-        form_angles(p, sc, t0, here);
-        __syncthreads();
-        int t = 0, h = threadIdx.x / lanes;
-        for (;; h += groups) {
-            for (; h >= n.r.H; h -= n.r.H) ++t;
-            if (t >= here) break;
-            const int64_t tok = t0 + t;
-            if (p.positions[tok] < 0) continue;
+        while (rows.t0 == t0) {
             float x[NI][2][VEC], g[NI][2][VEC], hw[NI][2][VEC];
-            lane.load((const E *)p.dout + tok * p.dout_token + h * p.dout_head, g);
-            lane.load((const E *)n.r.x + tok * n.r.x_token + h * n.r.x_head, x);
-            lane.rotate(g, sc + t * half, p.rot, n.r.rot_begin, -1.f);
+            lane.widen(raw_x, x);
+            lane.widen(raw_g, g);
+            const int64_t tok = rows.token();
+            const int t = rows.t, h = rows.h;
+            const bool there = position >= 0;
+            rows.next();
+            ask();
+            if (!there) continue;
+            lane.rotate(g, table + t * half, p.rot, n.r.rot_begin, -1.f);
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
@@ -275,22 +341,27 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(const NormParam
     }
 }
 
-// dw of 64 columns: 16 waves add every 16th partial sum each, in 64 bits, and then the 16 sums in their order.
+// dw of 16 columns: 64 rows of threads add every 64th partial sum each, in 64 bits, and then these in a fixed order.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *__restrict__ partial, float *__restrict__ dw, int n, int norm_dim)
 {
-    __shared__ double s_sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    __shared__ double s_sum[16][16];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), wave = threadIdx.x >> 6;
     double sum = 0;
     if (c < norm_dim) {
-#pragma unroll 16
-        for (int i = wave; i < n; i += 16) sum += (double)partial[(int64_t)i * norm_dim + c];
+#pragma unroll 12
+        for (int i = threadIdx.x >> 4; i < n; i += 64) sum += (double)partial[(int64_t)i * norm_dim + c];
     }
-    s_sum[wave][lane] = sum;
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if ((threadIdx.x & 63) < 16) s_sum[wave][threadIdx.x & 15] = sum;
     __syncthreads();
-    if (wave != 0 || c >= norm_dim) return;
-    for (int i = 1; i < 16; ++i) sum += s_sum[i][lane];
+    if (threadIdx.x >= 16 || c >= norm_dim) return;
+    sum = 0;
+    for (int i = 0; i < 16; ++i) sum += s_sum[i][threadIdx.x];
     dw[c] = (float)sum;
 }
+
+constexpr int kNormGroups = 2048;      // workgroups of queries, and of keys, at most
 
 // Lanes of a group: a power of two, at least 4; more than 64 items take several a lane.
 template <int VEC, bool PAIRS>
@@ -308,11 +379,12 @@ hipError_t launch_t(NormParams p, hipStream_t stream)
     constexpr int NI = VEC == 8 ? 1 : VEC == 4 ? 2 : 8;              // 1,024 columns are 64, 128 and 512 items
     p.q.lanes = p.q.r.H ? lanes_of<VEC, PAIRS>(p.q, p.rot, p.interleaved) : 64;
     p.k.lanes = p.k.r.H ? lanes_of<VEC, PAIRS>(p.k, p.rot, p.interleaved) : 64;
-    // as many tokens a workgroup as give each group of lanes a head
+    // Tokens of a chunk: as many as give each group of lanes a head, and each thread an angle, where that leaves a thousand chunks
     auto fill = [](const NormHeads &n) { return n.r.H ? (256 / n.lanes + n.r.H - 1) / n.r.H : 1; };
-    int tokens = fill(p.q) > fill(p.k) ? fill(p.q) : fill(p.k);
-    if (p.T <= 1024) tokens = 1;
-    const size_t lds = (size_t)tokens * (p.rot / 2) * sizeof(float2);
+    const int half = p.rot / 2, heads = fill(p.q) > fill(p.k) ? fill(p.q) : fill(p.k), angles = half < 16 ? 16 : (256 + half - 1) / half;
+    int tokens = p.T <= 1024 ? 1 : heads;
+    if (tokens < angles && p.T / 1024 > tokens) tokens = p.T / 1024 < angles ? (int)(p.T / 1024) : angles;
+    const size_t lds = (size_t)2 * tokens * half * sizeof(float2);
     const int64_t bytes = p.T * p.q.r.H * p.q.r.d * (int64_t)sizeof(E);
     const bool past = VEC > 1 && p.k.r.H == 0 && bytes >= 32 << 20;
     const int64_t blocks = (p.T + tokens - 1) / tokens;
@@ -324,11 +396,11 @@ hipError_t launch_t(NormParams p, hipStream_t stream)
         else hipLaunchKernelGGL((norm_rope_backward_kernel<E, VEC, PAIRS, NI, false>), dim3((unsigned)n), dim3(256), lds, stream, p, tokens);
         if (dw == nullptr || n == 1) return hipGetLastError();
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((p.q.norm_dim + 63) / 64)), dim3(1024), 0, stream, (const float *)p.partial, dw, n, p.q.norm_dim);
+        hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((p.q.norm_dim + 15) / 16)), dim3(1024), 0, stream, (const float *)p.partial, dw, n, p.q.norm_dim);
         return hipGetLastError();
     }
-    const int q_groups = p.q.r.H ? (int)blocks : 0;
-    const dim3 grid((unsigned)(q_groups + (p.k.r.H ? blocks : 0)));
+    const int most = (int)(blocks < kNormGroups ? blocks : kNormGroups), q_groups = p.q.r.H ? most : 0;
+    const dim3 grid((unsigned)(q_groups + (p.k.r.H ? most : 0)));
     if (past) hipLaunchKernelGGL((norm_rope_kernel<E, VEC, PAIRS, NI, true>), grid, dim3(256), lds, stream, p, tokens, q_groups);
     else hipLaunchKernelGGL((norm_rope_kernel<E, VEC, PAIRS, NI, false>), grid, dim3(256), lds, stream, p, tokens, q_groups);
     return hipGetLastError();
@@ -357,27 +429,8 @@ hipError_t launch_norm_rope(const NormParams &p, int elem_bytes, hipStream_t str
     const bool wide = heads(p.q) && heads(p.k) && whole(p.interleaved ? p.rot : p.rot / 2) &&
                       (p.v == nullptr || (at16(p.v) && at16(p.v_rows) && whole(p.v_token) && whole(p.v_head) && whole(p.d_v))) &&
                       (p.dout == nullptr || (at16(p.dout) && whole(p.dout_token) && whole(p.dout_head)));
-    auto go = [&](const NormParams &part) {
-        return elem_bytes == 2 ? (wide ? launch_v<uint16_t, 8>(part, stream) : launch_v<uint16_t, 1>(part, stream))
-                               : (wide ? launch_v<float, 4>(part, stream) : launch_v<float, 1>(part, stream));
-    };
-    if (p.dout) return go(p);                                        // (its workgroups go on until no token is left)
-    // (a launch has fewer than 2^32 threads in x: 2^22 workgroups each of queries and of keys, and calls of more tokens in parts)
-    constexpr int64_t kMostTokens = 1 << 22;
-    NormParams part = p;
-    for (int64_t t0 = 0; t0 < p.T; t0 += kMostTokens) {
-        auto from = [&](const void *x, int64_t token) { return x ? (const char *)x + t0 * token * elem_bytes : nullptr; };
-        part.T = p.T - t0 < kMostTokens ? p.T - t0 : kMostTokens;
-        part.q.r.x = from(p.q.r.x, p.q.r.x_token);
-        part.q.r.out = (void *)from(p.q.r.out, p.q.r.out_token);
-        part.k.r.x = from(p.k.r.x, p.k.r.x_token);                   // (rows of the cache are by slot)
-        part.v = from(p.v, p.v_token);
-        part.positions = p.positions + t0;
-        part.slots = p.slots ? p.slots + t0 : nullptr;
-        const hipError_t e = go(part);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    if (elem_bytes == 2) return wide ? launch_v<uint16_t, 8>(p, stream) : launch_v<uint16_t, 1>(p, stream);
+    return wide ? launch_v<float, 4>(p, stream) : launch_v<float, 1>(p, stream);
 }
 
 }  // namespace loza

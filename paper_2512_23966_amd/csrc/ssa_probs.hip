@@ -631,13 +631,13 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
 
 }  // namespace
 
-constexpr int kRows = 256;
-
-// Slices of a row: 2,048 workgroups in all, as far as there are 2,048 tokens for each.
+// A workgroup a row where there are many rows or they are short (up to 12,288 tokens, a row a 256 tokens, 256 rows), else slices: 2,048 workgroups in all as far as
+// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 9.9 and 11.9, 512 rows 18 and 30; 32,003,
+// 1 row 20 and 12, 64 rows 22.0 and 16.7, 128 rows 24 and 29; 131,072, 1 row 56 and 12, 192 rows 68 and 62, 256 rows 72 and 76, 512 rows 116 and 122.
 void probs_plan(ProbsParams &p)
 {
     const int64_t rows = (int64_t)p.B * p.n;
-    int64_t slices = rows >= kRows ? 1 : (2048 + rows - 1) / rows;
+    int64_t slices = rows >= 256 || rows * 256 >= p.V || p.V <= 12288 ? 1 : (2048 + rows - 1) / rows;
     const int64_t most = ((int64_t)p.V + kStep - 1) / kStep, least = ((int64_t)p.V + kMostSlice - 1) / kMostSlice;
     if (slices > most) slices = most;
     if (slices < least) slices = least;
@@ -651,7 +651,7 @@ static hipError_t launch_probs_t(const ProbsParams &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)((int64_t)p.B * p.n * p.slices));
     const size_t lds = p.masks || p.n_bias || p.allowed ? (size_t)(p.slice_len < p.V ? p.slice_len : p.V + 31) / 32 * 4 : 0;
-    if (p.slices == 1 && p.V > kStep) {
+    if (p.slices == 1) {
         hipLaunchKernelGGL((token_row_kernel<E, PLAIN, NT>), grid, dim3(kRowThreads), lds, stream, p);
         return hipGetLastError();
     }

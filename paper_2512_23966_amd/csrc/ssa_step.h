@@ -51,7 +51,7 @@ struct NormHeads {
     int norm_begin, norm_dim;
     int lanes;                    // of the group that takes a head (the launch's)
 };
-constexpr int kNormPartials = 1024;   // partial sums of a weight's gradient, at most
+constexpr int kNormPartials = 768;    // partial sums of a weight's gradient, at most: workgroups, three of which fit a compute unit
 struct NormParams {
     NormHeads q, k;               // k.r.H == 0: q alone; else k.r.out is the cache, row slots[t] of it
     const void *v;

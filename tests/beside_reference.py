@@ -59,7 +59,7 @@ def norm_rope_backward_bounds(dout, x, weight, begin, dim, eps, positions, freq,
     """G: m (|a| + |b|) for rotated columns, |dout| for others; g is off by 8 units of it at most, h = g w by 9, h x by 10. Their mean is added up in 24 steps
     and rounded twice more: 36 units of A = mean(G |w| |x|). r^2 is off by 31 (r by 15), the product with x by 3 more: x r^2 mean(h x) by 70 units of
     |x| r^2 A. Their difference, and the product with r: 9 + 1 + 16 and 70 + 1 + 16 units. dweight: 8 + 15 + 2 a term, and an addition for every row of a
-    workgroup (at most 64 and one 1,024th of the tokens) and every group of lanes (at most 64)."""
+    workgroup (at most 64 and one 768th of the tokens) and every group of lanes (at most 64)."""
     live = np.asarray(positions) >= 0
     first, second = _pairs(rot_begin, len(freq), interleaved)
     G = np.abs(dout)
@@ -71,7 +71,7 @@ def norm_rope_backward_bounds(dout, x, weight, begin, dim, eps, positions, freq,
     bound = 8 * U * G
     bound[..., cols] = U * r * (26 * Gn * w + 87 * xn * r ** 2 * A)
     T, H, _ = x.shape
-    terms = 25 + 64 + (T / 1024 + 64) * H
+    terms = 25 + 64 + (T / 768 + 64) * H
     return bound + half * np.abs(dx) + 1e-38, terms * U * (Gn * xn * r)[live].sum((0, 1)) + 1e-38
 
 
