@@ -58,6 +58,7 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(const ForkParams p)
     __shared__ int64_t s_sum[4];
     const int b = blockIdx.x, tid = threadIdx.x;
     const int64_t count = valid_count(p.free_count, p.num_free);
+    const Fork f = fork_of(p, b);                  // (asked for before there is anything to wait for)
     int64_t before = 0;
     const int upto = b == 0 ? p.B : b;             // (the first one adds up all, for what is left)
     for (int i = tid; i < upto; i += 256) before += fork_of(p, i).need;
@@ -69,7 +70,6 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(const ForkParams p)
         if (tid == 0) p.free_left[0] = (int32_t)(count - (before < count ? before : count));
         before = 0;
     }
-    const Fork f = fork_of(p, b);
     const bool ok = f.fits && (f.need == 0 || before < count);
     const int64_t full = ok ? f.rows >> p.page_shift : 0;
     int64_t first = 0;                             // pages of the source from here on, and those of the sink, are still its own
@@ -231,12 +231,13 @@ __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
 {
     __shared__ int64_t s_sum[16];
     __shared__ int32_t s_scan[16];
-    const int64_t count = valid_count(p.free_count, p.num_free), before = bits_below(p.freed, (int64_t)blockIdx.x * kPageGroup, s_sum);
-    const int64_t page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4;
+    const int64_t count = valid_count(p.free_count, p.num_free), page0 = (int64_t)blockIdx.x * kPageGroup + threadIdx.x * 4;
     int left[4], mine = 0;
 #pragma unroll
+    for (int k = 0; k < 4; ++k) left[k] = page0 + k < p.num_pages ? p.left[page0 + k] : 0;
+    const int64_t before = bits_below(p.freed, (int64_t)blockIdx.x * kPageGroup, s_sum);
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
-        left[k] = page0 + k < p.num_pages ? p.left[page0 + k] : 0;
         mine += left[k] < 0;
         if (p.shared && page0 + k < p.num_pages) p.shared_after[page0 + k] = left[k] < 0 ? 0 : left[k];
     }
