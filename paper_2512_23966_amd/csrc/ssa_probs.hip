@@ -335,20 +335,20 @@ struct Slice {
         if (x < 0) return false;
         const int z = seen ? seen[x] : 0;
         const bool ok = !allowed || (allowed[x >> 3] >> (x & 7) & 1);
-        const float *values = p.bias_values + (int64_t)b * p.n_bias - nodes;
+        const float *values = p.bias_values + (int64_t)b * p.n_bias;
         int said = z & 0x7fff, first = i;
         float bias = 0.f;
         l = Elem<E>::get(row[x]);
         if (!again) {
             if (i < nodes) ++said;
-            else bias = values[i];
+            else bias = values[i - nodes];
         } else {
 #pragma unroll 8
             for (int k = 0; k < entries; ++k) {
                 if (tok[k] != x) continue;
                 if (k < first) first = k;
                 if (k < nodes) ++said;
-                else bias = add(bias, values[k]);
+                else bias = add(bias, values[k - nodes]);
             }
         }
         const bool occurred = z >= 0x8000 || said > 0;
@@ -418,45 +418,64 @@ __device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, PLAIN> &s,
     return a;
 }
 
-// The probabilities of a slice, given the Stat of its row
-template <bool NT, bool SOFT, typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ void write_probs_t(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, const Weight &w)
+// 8 results of a lane. (Two stores written out: one in either branch of a condition is merged to a plain one.)
+template <bool NT>
+__device__ __forceinline__ void store_unit(float *out, int x, int V, bool whole, const float (&l)[kUnit])
+{
+    if (whole) {
+        typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+        u32x4 y[2];
+        __builtin_memcpy(y, l, sizeof(y));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if constexpr (NT) __builtin_nontemporal_store(y[k], (u32x4_at4 *)(out + x + kHalf * k));
+            else *(u32x4_at4 *)(out + x + kHalf * k) = y[k];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i)
+            if (token_of(x, i) < V) out[token_of(x, i)] = l[i];
+    }
+}
+
+// The probabilities of a slice of a row that is not greedy, given the row's Stat
+template <bool NT, typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ void write_soft(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, const Weight &w)
 {
     const float inv = a.m == LOZA_NEG_INF ? 0.f : 1.f / a.s;
     const bool infinite = a.m == __builtin_inff() || a.m == LOZA_NEG_INF;       // (nothing weighs: 0 for all)
-    auto prob = [&](float l, int x) { return SOFT ? w(l - a.m) * inv : x == a.x ? 1.f : 0.f; };
     auto rare = [&](float l) { return l == a.m ? inv : 0.f; };
     s.units([&](int x, const Raw<E> &raw, bool whole) {
         float l[kUnit];
-        s.template changed<SOFT>(x, whole, raw, l);
-        if (SOFT && infinite) {
+        s.template changed<true>(x, whole, raw, l);
+        if (infinite) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) l[i] = rare(l[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) l[i] = prob(l[i], token_of(x, i));
+            for (int i = 0; i < kUnit; ++i) l[i] = w(l[i] - a.m) * inv;
         }
-        if (whole) {
-            // (those done apart are overwritten below)
-            typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
-            u32x4 y[2];
-            __builtin_memcpy(y, l, sizeof(y));
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if constexpr (NT) __builtin_nontemporal_store(y[k], (u32x4_at4 *)(out + x + kHalf * k));
-                else *(u32x4_at4 *)(out + x + kHalf * k) = y[k];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i)
-                if (token_of(x, i) < s.p.V) out[token_of(x, i)] = l[i];
-        }
+        store_unit<NT>(out, x, s.p.V, whole, l);
     });
     if (PLAIN || s.entries == 0) return;
+    // those done apart, over what the pass wrote there
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));                        // this wave's are written
     __syncthreads();
     for (int i = threadIdx.x; i < s.entries; i += THREADS)
-        if (s.tok[i] >= 0) out[s.tok[i]] = SOFT && infinite ? rare(s.val[i]) : prob(s.val[i], s.tok[i]);
+        if (s.tok[i] >= 0) out[s.tok[i]] = infinite ? rare(s.val[i]) : w(s.val[i] - a.m) * inv;
+}
+
+// ... of a greedy one: nothing is read again
+template <bool NT, typename E, int THREADS, bool PLAIN>
+__device__ __forceinline__ void write_greedy(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a)
+{
+    for (int at = s.x0 + (int)(threadIdx.x >> 6) * kBlock; at < s.x1; at += THREADS * kUnit) {
+        const int x = at + 4 * (threadIdx.x & 63);
+        float l[kUnit];
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) l[i] = token_of(x, i) == a.x ? 1.f : 0.f;
+        store_unit<NT>(out, x, s.p.V, at + kBlock <= s.x1, l);
+    }
 }
 
 template <typename E, int THREADS, bool PLAIN>
@@ -467,8 +486,8 @@ __device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS, PLAIN> &s, f
 template <bool NT, typename E, int THREADS, bool PLAIN>
 __device__ __forceinline__ void write_probs(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, float t, const Weight &w)
 {
-    if (t > 0.f) write_probs_t<NT, true>(s, out, a, w);
-    else write_probs_t<NT, false>(s, out, a, w);
+    if (t > 0.f) write_soft<NT>(s, out, a, w);
+    else write_greedy<NT>(s, out, a);
 }
 
 // Whether a row is one of its tree's
