@@ -436,8 +436,10 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  * The step around the attention: what an engine that drafts tokens calls between one decode step and the next, all of
  * it on the GPU (no lengths on the host), so that a step can be captured. The paper stretches its contexts with YaRN and
  * measures its kernels inside such an engine (Training and Efficiency sections); it describes none of this, the definitions
- * are the usual ones. A step: loza_ssa_step_tables_held, then in every layer loza_ssa_rope_append and loza_ssa_extend_tree
- * (or loza_ssa_decode_paged, loza_ssa_extend_paged), then loza_ssa_verify_tree, and loza_ssa_keep_accepted for all layers.
+ * are the usual ones. A step: loza_ssa_step_tables_held, then in every layer loza_ssa_rope_append (models that norm their queries and keys:
+ * loza_ssa_norm_rope_append) and loza_ssa_extend_tree (or loza_ssa_decode_paged, loza_ssa_extend_paged), then loza_ssa_token_probs and
+ * loza_ssa_verify_tree, loza_ssa_keep_accepted for all layers and loza_ssa_count_tokens; requests are forked (loza_ssa_pages_fork, loza_ssa_pages_copy) and
+ * their pages given back (loza_ssa_pages_free) between steps.
  *
  * Trees. The tokens of a step are the nodes of a tree per sequence, at most LOZA_TREE_MAX_NODES of them, parents before their
  * children. parents[b, r] is the parent of node r, an index below r; anything else: a node without a parent. Node 0 is the
@@ -450,7 +452,7 @@ int64_t loza_ssa_live_pairs_blocks(int64_t S, int64_t sink_blocks, int64_t local
  * the pages [ceil((cache_len + path_len) / page_size), ceil(seqlen / page_size)) of each row back itself, or they are lost). An engine whose requests
  * take both, chunks and drafts, tells it with both. Between two steps: cache_lens += path_lens (chunks: granted), free_count = free_left, held = held_after.
  * A request that ends has the first `held` entries of its row appended to free_pages from free_count on (which has room for every page), free_count grows by
- * as many, and its cache_len and held are 0.
+ * as many, and its cache_len and held are 0 (loza_ssa_pages_free does that, also where requests share pages).
  */
 #define LOZA_TREE_MAX_NODES 64
 #define LOZA_ROPE_MAX_DIM 1024
@@ -539,7 +541,7 @@ int loza_ssa_rope_append_f32(const float *q, const float *k, const float *v, con
  * loza_ssa_rope rotates them. The two ranges may be apart (a latent row: 512 normed columns, 64 rotated ones), the same (heads of width 128), or overlap.
  *   weight [norm_dim] fp32, NULL: ones     1 <= norm_dim, d <= LOZA_NORM_MAX_DIM; eps: a positive normal number
  *   everything else, padding, strides and in-place calls among it: as loza_ssa_rope. A head whose squares add up to more than fp32 holds gives 0.
- * Sums in fp32, one rounding of each result. Arrays of which x and out are slices may differ; all heads have the one weight.
+ * Sums in fp32, one rounding of each result. All heads have the one weight.
  */
 #define LOZA_NORM_MAX_DIM 1024
 int loza_ssa_norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
@@ -666,7 +668,7 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
  *           those below tree_lens[b], were said as well, each once a node
  *   seen [B] rows, seen_row elements apart (a multiple of 8, >= V, < 2^31; 16-byte aligned), or NULL: what was said before the path (loza_ssa_count_tokens):
  *           bit 15 says that the token occurs in the prompt, the others how often it was said
- *   repetition (> 0; NULL: 1), frequency, presence (NULL: 0), temperature (NULL: 1) [B] fp32
+ *   repetition (2^-100 .. 2^100; NULL: 1), frequency, presence (NULL: 0), temperature (NULL: 1) [B] fp32
  *   bias_tokens [B, n_bias] int32, bias_values [B, n_bias] fp32 (n_bias <= LOZA_MAX_BIAS; tokens outside [0, V) are skipped, those of one token add up in order)
  *   allowed [B, n, ceil(V / 32)] int32 or NULL: bit x % 32 of word x / 32 says that token x may come
  *   workspace: loza_ssa_token_probs_workspace_bytes, 16-byte aligned; contents ignored; two calls that overlap in time need two
@@ -695,7 +697,7 @@ int loza_ssa_token_probs_f32(const float *logits, int64_t logits_row, const int3
  *   lens [B] int32 (cut to [0, n]), prompt_lens [B] int32 or NULL (none)
  *   fresh [B] int32 or NULL: where it is not 0, the request's row is cleared first (a new request, with its prompt and what it has said already)
  *   seen [B] rows, seen_row elements apart, as above
- * B <= 65535, n <= 2^30, V <= 2^30. The result does not depend on the order of the entries.
+ * B <= 65535, n <= 2^30, V <= 2^30. The result does not depend on the order of the entries. Two calls that overlap in time must not have rows of seen in common.
  */
 int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int32_t *lens, const int32_t *prompt_lens, const int32_t *fresh,
                           uint16_t *seen, int64_t seen_row, int B, int n, int V, void *stream);
