@@ -33,6 +33,7 @@ constexpr int kMostSpecial = kTreeNodes + kMostBias;
 struct Change {
     float rep, inv, inv_lo, fre, pre;  // inv + inv_lo: 1 / rep
     bool quick;                        // the division by `rep` as below
+    bool repeats, counts, occurs;      // which of the three change anything: requests rarely ask for all of them (20,000 of 131,072 tokens said, 1,024 rows: PLACEHOLDER)
 
     __device__ __forceinline__ void set(float rep_, float fre_, float pre_)
     {
@@ -42,11 +43,44 @@ struct Change {
         fre = fre_;
         pre = pre_;
         quick = rep >= 0x1p-100f && rep <= 0x1p100f;
+        repeats = rep_ != 1.f;
+        counts = fre_ != 0.f;
+        occurs = pre_ != 0.f || !(fabsf(fre_) < __builtin_inff());   // (infinity times 0 is not 0)
     }
     __device__ __forceinline__ float soft(float l, bool occurred, uint32_t said) const
     {
-        const float r = l * (l > 0.f ? inv : rep), less = said != 0 ? __builtin_fmaf(fre, (float)said, pre) : 0.f;
-        return (occurred ? r : l) - less;
+        const float less = said != 0 ? __builtin_fmaf(fre, (float)said, pre) : 0.f;
+        return __builtin_fmaf(l, factor(l, occurred), -less);
+    }
+    __device__ __forceinline__ float factor(float l, bool occurred) const
+    {
+        const float f = l > 0.f ? inv : rep;
+        return occurred ? f : 1.f;
+    }
+    // The same of a lane's tokens, z(i) the record of the i-th
+    template <typename F>
+    __device__ __forceinline__ void soft(float (&l)[kUnit], F z) const
+    {
+        float less[kUnit] = {};
+        if (!occurs) {
+            if (counts) {
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) less[i] = fre * (float)(z(i) & 0x7fffu);
+            }
+        } else if (!counts) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) less[i] = (z(i) & 0x7fffu) != 0 ? pre : 0.f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) less[i] = (z(i) & 0x7fffu) != 0 ? __builtin_fmaf(fre, (float)(z(i) & 0x7fffu), pre) : 0.f;
+        }
+        if (repeats) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) l[i] = __builtin_fmaf(l[i], factor(l[i], z(i) != 0), -less[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) l[i] -= less[i];
+        }
     }
     __device__ __forceinline__ float rounded(float l, bool occurred, uint32_t said) const
     {
@@ -59,16 +93,32 @@ struct Change {
         }
         return l;
     }
-    // The same without branches. l / rep as l (inv + inv_lo), which is off by less than a unit, and a correction by what is left, fma(-q, rep, l) inv: that gives
+    // The same without branches of lanes. l / rep as l (inv + inv_lo), which is off by less than a unit, and a correction by what is left, fma(-q, rep, l) inv: that gives
     // the rounded quotient (Markstein 1990; below 2^-100 it may miss by a step). One that overflows comes out as a NaN.
-    __device__ __forceinline__ float quickly(float l, bool occurred, uint32_t said) const
+    template <typename F>
+    __device__ __forceinline__ void quickly(float (&l)[kUnit], F z) const
     {
 #pragma clang fp contract(off)
-        float q = __builtin_fmaf(l, inv_lo, l * inv);
-        q = __builtin_fmaf(__builtin_fmaf(-q, rep, l), inv, q);
-        const float r = __builtin_amdgcn_classf(l, 0x180) ? q : l * rep;         // (positive and finite)
-        const float was = occurred ? r : l, f = fre * (float)said, less = (was - f) - pre;
-        return said != 0 ? less : was;
+        if (repeats) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) {
+                float q = __builtin_fmaf(l[i], inv_lo, l[i] * inv);
+                q = __builtin_fmaf(__builtin_fmaf(-q, rep, l[i]), inv, q);
+                const float r = __builtin_amdgcn_classf(l[i], 0x180) ? q : l[i] * rep;         // (positive and finite)
+                l[i] = z(i) != 0 ? r : l[i];
+            }
+        }
+        if (counts) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) {
+                const float f = fre * (float)(z(i) & 0x7fffu);       // (0 where the token was not said)
+                l[i] -= f;
+            }
+        }
+        if (occurs) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) l[i] -= (z(i) & 0x7fffu) != 0 ? pre : 0.f;
+        }
     }
 };
 
@@ -140,10 +190,11 @@ __device__ __forceinline__ float add(float a, float b)
     return a + b;
 }
 
-// The tokens that are done apart, in LDS
+// The tokens that are done apart, in LDS: those of a block of 512 as a list from first[block] on, -1 at its end
 struct Special {
     int32_t tok[kMostSpecial], again;
     float val[kMostSpecial];
+    int32_t first[kMostSlice / kBlock], next[kMostSpecial];
 };
 
 // One row's slice [x0, x1): the tokens that are done apart, and what the pass over the others needs. PLAIN: there are no such tokens, no record and no grammar.
@@ -157,11 +208,10 @@ struct Slice {
     uint32_t bits_mine = 0;       // which of this thread's entries stand for their tokens (1,088 entries are at most 5 a thread)
     Change change;
     bool soft;
-    int32_t *tok;                 // LDS: [entries] tokens done apart, -1 where they are not in the slice
-    float *val;                   // LDS: their changed logits
+    Special &lds;                 // tok: tokens done apart, -1 where they are not in the slice; val: their changed logits
     uint32_t *bits;               // LDS: a bit a token of the slice: done apart, or not allowed
 
-    __device__ __forceinline__ Slice(const ProbsParams &p_, int64_t row_index, int slice, Special &lds, uint32_t *bits_) : p(p_), tok(lds.tok), val(lds.val), bits(bits_)
+    __device__ __forceinline__ Slice(const ProbsParams &p_, int64_t row_index, int slice, Special &lds_, uint32_t *bits_) : p(p_), lds(lds_), bits(bits_)
     {
         b = (int)(row_index / p.n);
         r = (int)(row_index - (int64_t)b * p.n);
@@ -183,19 +233,16 @@ struct Slice {
             bar(words);
             return;
         }
+        uint64_t path = nodes ? (uint64_t)p.masks[row_index] : 0;    // (nodes before the tree's end)
+        if (nodes) path &= length() >= 64 ? ~0ull : (1ull << (length() > 0 ? length() : 0)) - 1;
         for (int i = threadIdx.x; i < words; i += THREADS) bits[i] = 0;
+        for (int i = threadIdx.x; i < (x1 - x0 + kBlock - 1) / kBlock; i += THREADS) lds.first[i] = -1;
         if (threadIdx.x == 0) lds.again = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < entries; i += THREADS) {
-            int x = -1;
-            if (i < nodes) {
-                const uint64_t path = (uint64_t)p.masks[row_index];
-                if ((path >> i & 1) && i < length()) x = p.tokens[(int64_t)b * p.n + i];
-            } else {
-                x = p.bias_tokens[(int64_t)b * p.n_bias + i - nodes];
-            }
-            if (x < x0 || x >= x1) x = -1;
-            tok[i] = x;
+            int x = i < nodes ? p.tokens[(int64_t)b * p.n + i] : p.bias_tokens[(int64_t)b * p.n_bias + i - nodes];
+            if (x < x0 || x >= x1 || (i < nodes && !(path >> i & 1))) x = -1;
+            lds.tok[i] = x;
             if (x >= 0) {
                 const uint32_t bit = 1u << ((x - x0) & 31);
                 if (atomicOr(&bits[(x - x0) >> 5], bit) & bit) lds.again = 1;
@@ -207,14 +254,13 @@ struct Slice {
         for (int i = threadIdx.x; i < entries; i += THREADS) {
             float l = 0.f;
             const bool mine = special(i, again, l);
-            val[i] = l;
-            if (!again && !mine) tok[i] = -1;
-            if (again) bits_mine = mine ? bits_mine | 1u << (i / THREADS) : bits_mine;
+            lds.val[i] = l;
+            if (mine) bits_mine |= 1u << (i / THREADS);
         }
-        if (again) {
-            __syncthreads();                                          // (all have looked at the list)
-            for (int i = threadIdx.x; i < entries; i += THREADS)
-                if (!(bits_mine >> (i / THREADS) & 1)) tok[i] = -1;
+        if (again) __syncthreads();                                   // (all have looked at the tokens)
+        for (int i = threadIdx.x; i < entries; i += THREADS) {
+            if (bits_mine >> (i / THREADS) & 1) lds.next[i] = atomicExch(&lds.first[(lds.tok[i] - x0) / kBlock], i);
+            else lds.tok[i] = -1;
         }
         bar(words);
     }
@@ -235,10 +281,11 @@ struct Slice {
     __device__ __forceinline__ void load(int x, bool whole, Raw<E> &raw) const
     {
         constexpr int W = Raw<E>::kWords;
-        raw.ok = 0;
+        raw.ok = ok_of(x, whole);
+        if (!PLAIN && !__any(raw.ok != 0)) return;                   // (none of 512 tokens is allowed)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;  // tokens of this half that are there
+            const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;
             raw.z[2 * h] = raw.z[2 * h + 1] = 0;
             if (!whole && n < 4) {
                 E e[4] = {};
@@ -255,33 +302,47 @@ struct Slice {
                 raw.z[2 * h] = z[0];
                 raw.z[2 * h + 1] = z[1];
             }
+        }
+    }
+    // Which of a lane's tokens are there, allowed and not done apart
+    __device__ __forceinline__ uint32_t ok_of(int x, bool whole) const
+    {
+        uint32_t all = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;
+            if (n <= 0) continue;
             uint32_t ok = 15u;
             if (!PLAIN && (entries || allowed)) ok = ~((uint32_t)((const uint8_t *)bits)[(xh - x0) >> 3] >> (xh & 4)) & 15u;
             if (!whole && n < 4) ok &= (1u << n) - 1;
-            raw.ok |= ok << (4 * h);
+            all |= ok << (4 * h);
         }
+        return all;
     }
     // Their changed logits; -inf for those done apart, not allowed, or not there
     template <bool SOFT>
     __device__ __forceinline__ void changed(int x, bool whole, const Raw<E> &raw, float (&l)[kUnit]) const
     {
+        if (!PLAIN && !__any(raw.ok != 0)) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) l[i] = LOZA_NEG_INF;
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kUnit; ++i) l[i] = raw.logit(i);
         // (branches of whole waves: a branch of lanes has the compiler keep a copy of everything)
         bool again = false;
         if (!PLAIN && __any((raw.z[0] | raw.z[1] | raw.z[2] | raw.z[3]) != 0)) {
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) {
-                const uint32_t z = raw.record(i);
-                l[i] = SOFT ? change.soft(l[i], z != 0, z & 0x7fffu) : change.quickly(l[i], z != 0, z & 0x7fffu);
-            }
+            auto z = [&](int i) { return raw.record(i); };
+            if constexpr (SOFT) change.soft(l, z);
+            else change.quickly(l, z);
             again = !SOFT && !change.quick;
         }
-        // (two a comparison)
-        bool nans = again;
+        // (two a comparison, in scalar registers: as a condition of lanes it is 16 instructions)
+        uint64_t nans = 0;
 #pragma unroll
-        for (int i = 0; i < kUnit; i += 2) nans |= __builtin_isunordered(l[i], l[i + 1]);
-        if (__any(nans)) {
+        for (int i = 0; i < kUnit; i += 2) nans |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(l[i], l[i + 1]));
+        if (again || nans) {
             if (PLAIN || SOFT) {
 #pragma unroll
                 for (int i = 0; i < kUnit; ++i) l[i] = settle(l[i]);
@@ -329,10 +390,12 @@ struct Slice {
             f(at + lane4, raw, whole);
         }
     }
+    // An entry of a list, the same for the whole wave
+    __device__ __forceinline__ static int list(const int32_t *of, int i) { return __builtin_amdgcn_readfirstlane(of[i]); }
     // The changed logit of entry i, and whether it is the one that stands for its token; `again`: some token is there more than once
     __device__ __forceinline__ bool special(int i, bool again, float &l) const
     {
-        const int x = tok[i], nodes = p.masks ? p.n : 0;
+        const int x = lds.tok[i], nodes = p.masks ? p.n : 0;
         if (x < 0) return false;
         const int z = seen ? seen[x] : 0;
         const bool ok = !allowed || (allowed[x >> 3] >> (x & 7) & 1);
@@ -346,7 +409,7 @@ struct Slice {
         } else {
 #pragma unroll 8
             for (int k = 0; k < entries; ++k) {
-                if (tok[k] != x) continue;
+                if (lds.tok[k] != x) continue;
                 if (k < first) first = k;
                 if (k < nodes) ++said;
                 else bias = add(bias, values[k - nodes]);
@@ -415,7 +478,7 @@ __device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, PLAIN> &s,
     });
     if constexpr (!PLAIN)
         for (int i = threadIdx.x; i < s.entries; i += THREADS)
-            if (s.tok[i] >= 0) merge(a, s.val[i], 1.f, s.tok[i], w);
+            if (s.lds.tok[i] >= 0) merge(a, s.lds.val[i], 1.f, s.lds.tok[i], w);
     return a;
 }
 
@@ -456,14 +519,17 @@ __device__ __forceinline__ void write_soft(const Slice<E, THREADS, PLAIN> &s, fl
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) l[i] = w(l[i] - a.m) * inv;
         }
+        if (!PLAIN && s.entries) {
+            // those done apart, into what is stored (single words behind it took 10 us of 170 for 64 of them in each of 853 rows)
+            for (int e = s.list(s.lds.first, (x - s.x0) / kBlock); e >= 0; e = s.list(s.lds.next, e)) {
+                const int at = s.lds.tok[e] - x;
+                const float y = infinite ? rare(s.lds.val[e]) : w(s.lds.val[e] - a.m) * inv;
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) l[i] = at == token_of(0, i) ? y : l[i];
+            }
+        }
         store_unit<NT>(out, x, s.p.V, whole, l);
     });
-    if (PLAIN || s.entries == 0) return;
-    // those done apart, over what the pass wrote there
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));                        // this wave's are written
-    __syncthreads();
-    for (int i = threadIdx.x; i < s.entries; i += THREADS)
-        if (s.tok[i] >= 0) out[s.tok[i]] = infinite ? rare(s.val[i]) : w(s.val[i] - a.m) * inv;
 }
 
 // ... of a greedy one: nothing is read again
