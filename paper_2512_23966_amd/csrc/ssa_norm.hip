@@ -389,8 +389,9 @@ hipError_t launch_t(NormParams p, hipStream_t stream)
     int tokens = p.T <= 1024 ? 1 : heads;
     if (tokens < angles && p.T / 1024 > tokens) tokens = p.T / 1024 < angles ? (int)(p.T / 1024) : angles;
     const size_t lds = (size_t)2 * tokens * half * sizeof(float2);
-    const int64_t bytes = p.T * p.q.r.H * p.q.r.d * (int64_t)sizeof(E);
-    const bool past = VEC > 1 && p.k.r.H == 0 && bytes >= 32 << 20;
+    // From 16 MB on results are stored past the caches, which keep x for the gradient: forward and gradient, 16 MB 27 -> 24 us, 32 MB 41 -> 38, 64 MB 67 and 67, 128 MB
+    // 132 -> 122, 256 MB 264 -> 255. (What reads the forward's result next, an addition: 16 and 32 MB 22 -> 20 and 28 -> 28 us, 128 MB 86 -> 95, 256 MB 195 -> 199.)
+    const bool past = VEC > 1 && p.k.r.H == 0 && p.T > ((16 << 20) - 1) / ((int64_t)p.q.r.H * p.q.r.d * (int64_t)sizeof(E));
     const int64_t blocks = (p.T + tokens - 1) / tokens;
     if (p.dout) {
         const int n = (int)(blocks < kNormPartials ? blocks : kNormPartials);

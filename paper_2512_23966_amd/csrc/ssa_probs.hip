@@ -5,8 +5,8 @@
 //     l' = l / repetition if l > 0, l * repetition otherwise, where it occurred;  l'' = l' - frequency c - presence (c > 0) + bias
 // and no weight where the grammar does not allow it (or l'' is a NaN); p = exp((l'' - max) / T) / sum, or 1 at the first of the largest.
 //
-// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 155 us, 5.2 TB/s); with everything the vector
-// ALU, 46 instructions a token in two passes, 24 of them for the record, next to the memory's 135 us (the same, 853 of the rows alive: 215 us). All of it is done
+// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 155 us, 5.2 TB/s); with everything
+// (the same, 853 of the rows alive) 164 us, 137 of them the memory's, the vector ALU the rest: some 30 instructions a token in two passes, half of them for the record. All of it is done
 // on the way. The tokens of a tree's own nodes and the biased ones are a few hundred of 100,000: the pass over the row leaves
 // them out (a bit each in LDS), and a thread each does them apart, so that the pass looks nothing up.
 #include <hip/hip_runtime.h>
@@ -33,7 +33,7 @@ constexpr int kMostSpecial = kTreeNodes + kMostBias;
 struct Change {
     float rep, inv, inv_lo, fre, pre;  // inv + inv_lo: 1 / rep
     bool quick;                        // the division by `rep` as below
-    bool repeats, counts, occurs;      // which of the three change anything: requests rarely ask for all of them (20,000 of 131,072 tokens said, 1,024 rows: PLACEHOLDER)
+    bool repeats, counts, occurs;      // which of the three change anything: requests rarely ask for all of them (853 rows of 131,072, a sixth of them said: 215 -> 196 us)
 
     __device__ __forceinline__ void set(float rep_, float fre_, float pre_)
     {
@@ -658,12 +658,14 @@ __global__ __launch_bounds__(256) void count_tokens_kernel(const CountParams p)
 
 // The same for many tokens: a workgroup takes a slice of a request's row, counts in LDS (bit 31: in the prompt) what of all tokens falls into it, and
 // writes the units of 8 that changed. Every slice reads all tokens, out of L2.
-constexpr int kCountSlice = 16384, kCountThreads = 1024;
+constexpr int kCountSlice = 8192, kCountThreads = 1024;
 
 __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountParams p)
 {
     __shared__ uint32_t s_count[kCountSlice];
     const int b = blockIdx.y, x0 = blockIdx.x * kCountSlice;
+    const bool fresh = p.fresh && p.fresh[b] != 0;
+    if (p.lens[b] <= 0 && !fresh) return;
     for (int i = threadIdx.x; i < kCountSlice; i += kCountThreads) s_count[i] = 0;
     __syncthreads();
     int len = p.lens[b];
@@ -673,7 +675,7 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
     const uint32_t end = (uint32_t)(x0 >= p.V ? 0 : p.V - x0 < kCountSlice ? p.V - x0 : kCountSlice);     // (a row may be longer than the vocabulary)
     auto note = [&](int i, int x) {
         const uint32_t at = (uint32_t)(x - x0);                      // (tokens outside the slice, negative ones too, are large)
-        if (x < x0 || at >= end) return;
+        if (at >= end) return;
         if (i < prompt) atomicOr(&s_count[at], 0x80000000u);
         else atomicAdd(&s_count[at], 1u);                            // (fewer than 2^31 of them)
     };
@@ -683,11 +685,21 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
             if (at >= 0 && at < p.n) note(i, tokens[at]);
         }
     } else {
-#pragma unroll 4
-        for (int i = threadIdx.x * 4; i < len; i += kCountThreads * 4) {
+        constexpr int kAhead = 4, kPass = kCountThreads * 4;
+        int i = threadIdx.x * 4;
+        for (; i + (kAhead - 1) * kPass + 4 <= len; i += kAhead * kPass) {
+            i32x4 x[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) __builtin_memcpy(&x[a], tokens + i + a * kPass, 16);      // (rows of odd lengths are aligned to their elements only)
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) note(i + a * kPass + k, x[a][k]);
+        }
+        for (; i < len; i += kPass) {
             if (i + 4 <= len) {
                 i32x4 x;
-                __builtin_memcpy(&x, tokens + i, 16);                // (rows of odd lengths are aligned to their elements only)
+                __builtin_memcpy(&x, tokens + i, 16);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) note(i + k, x[k]);
             } else {
@@ -696,7 +708,6 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
         }
     }
     __syncthreads();
-    const bool fresh = p.fresh && p.fresh[b] != 0;
     uint16_t *row = p.seen + (int64_t)b * p.seen_row;
     for (int i = threadIdx.x * 8; i < kCountSlice; i += kCountThreads * 8) {
         if ((int64_t)x0 + i >= p.seen_row) break;
@@ -718,8 +729,8 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
 }  // namespace
 
 // A workgroup a row where there are many rows or they are short (up to 12,288 tokens, a row a 256 tokens, 256 rows), else slices: 2,048 workgroups in all as far as
-// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 9.9 and 11.9, 512 rows 18 and 30; 32,003,
-// 1 row 20 and 12, 64 rows 22.0 and 16.7, 128 rows 24 and 29; 131,072, 1 row 56 and 12, 192 rows 68 and 62, 256 rows 72 and 76, 512 rows 116 and 122.
+// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 10 and 13, 512 rows 19 and 28; 32,003,
+// 1 row 20 and 13, 64 rows 23 and 17, 128 rows 26 and 30; 131,072, 1 row 51 and 13, 192 rows 72 and 61, 256 rows 74 and 75, 512 rows 104 and 117.
 void probs_plan(ProbsParams &p)
 {
     const int64_t rows = (int64_t)p.B * p.n;
@@ -766,12 +777,14 @@ hipError_t launch_token_probs(const ProbsParams &p, int elem_bytes, hipStream_t 
     return elem_bytes == 2 ? launch_probs_e<uint16_t>(p, stream) : launch_probs_e<float>(p, stream);
 }
 
-constexpr int kManyTokens = 1024;
+// Entries by slices from here on, where the row is no longer than a million. 16 requests, us, an entry a thread and slices: 131,072 tokens, 64 entries 2.5 and 3.8, 512 of
+// them 3.5 and 4.2, 8,192 20 and 5; with one in 20 the same token 3.6 and 3.9, 12.9 and 4.1, 555 and 5. A million tokens, 512 entries 3 to 13 and 8; four million 3 to 13 and 21.
+constexpr int kManyTokens = 256;
 
 hipError_t launch_count_tokens(const CountParams &p, hipStream_t stream)
 {
     const int64_t slices = (p.seen_row + kCountSlice - 1) / kCountSlice;
-    if (p.n >= kManyTokens && slices <= 64) {
+    if (p.n >= kManyTokens && slices <= 128) {
         hipLaunchKernelGGL(count_slice_kernel, dim3((unsigned)slices, (unsigned)p.B), dim3(kCountThreads), 0, stream, p);
         return hipGetLastError();
     }

@@ -277,3 +277,72 @@ def test_count_stops_at_its_largest(gpu_device):
     assert seen[0].tolist() == [0, 0, 0, 32767, 0, 0, 0, 0]
     loza.loza_ssa_count_tokens(tokens, torch.tensor([n], dtype=I32, device=gpu_device), seen, 5, prompt_lens=torch.tensor([1], dtype=I32, device=gpu_device))
     assert seen[0].tolist() == [0, 0, 0, -1, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("B,V", [(1, 8191), (3, 8193), (2, 16_384), (2, 1_048_576), (1, 1_048_577)])
+@pytest.mark.parametrize("n", [255, 256, 4095, 4096, 16_385, 32_771])
+def test_count_around_its_steps(gpu_device, B, V, n):
+    """One entry a thread or slices of the vocabulary; loads of four, alone or four under way; requests of no entries, fresh or not."""
+    rng = np.random.default_rng(n + V)
+    row = (V + 7) // 8 * 8 + 16
+    seen = rng.choice(np.array([0, 0, 1, 0x8000, 0x7fff], np.uint16), size=(B, row))
+    tokens = rng.integers(-1, V + 1, size=(B, n)).astype(np.int32)
+    tokens[:, 0], tokens[:, -1], tokens[:, n // 2] = V - 1, -2 ** 31, 2 ** 31 - 1
+    lens = np.array([n, 0, n - 1][:B], np.int32)
+    prompt = np.array([n // 2, 5, n][:B], np.int32)
+    for fresh in (None, np.array([0, 1, 0][:B], np.int32), np.array([1, 0, 1][:B], np.int32)):
+        t = _dev(seen.view(np.int16), gpu_device)
+        loza.loza_ssa_count_tokens(_dev(tokens, gpu_device), _dev(lens, gpu_device), t, V, prompt_lens=_dev(prompt, gpu_device), fresh=_dev(fresh, gpu_device))
+        assert np.array_equal(t.cpu().numpy().view(np.uint16), N.count(seen, tokens, lens, V, None, prompt, fresh))
+
+
+# ---- penalties that change nothing, grammars that leave little, tokens done apart -----------------------------------------
+
+@pytest.mark.parametrize("temp", [0.0, 0.9])
+@pytest.mark.parametrize("rep", [1.0, 1.3, 0.7])
+@pytest.mark.parametrize("fre", [0.0, -0.0, 0.2, float("inf"), float("-inf")])
+@pytest.mark.parametrize("pre", [0.0, 0.4, float("inf")])
+def test_each_penalty_alone_and_together(gpu_device, pre, fre, rep, temp):
+    for dtype in (BF, F32):
+        c = Call(2, 3, 2600, dtype, 21)
+        for name, x in (("rep", rep), ("fre", fre), ("pre", pre), ("temp", temp)):
+            getattr(c, name)[:] = x
+        if np.isinf(fre) or np.isinf(pre):                  # (tokens that were said are sure or barred then: some have to be left)
+            c.seen[:, 1::2] = 0
+        c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,n,V", [(1, 2, 40_000), (4, 64, 5003), (2, 3, 9001)])
+def test_grammars_that_leave_little(gpu_device, B, n, V, dtype):
+    """Whole blocks of 512 tokens are barred, NaNs and infinities in them; what is left: one token, one of a tree's own, a biased one, the last ones."""
+    c = Call(B, n, V, dtype, 31)
+    c.ok[:] = False
+    c.ok[0, 0, 3] = True
+    c.ok[0, 1, int(c.tokens[0, 0])] = True
+    c.ok[-1, 0, int(c.bt[-1, 0])] = True
+    c.ok[-1, -1, V - 2:] = True
+    c.ok[-1, 1, 512:1024] = True
+    c.ok[-1, 1, 2048:2050] = True
+    c.temp[:] = [(0.0, 1.3)[b % 2] for b in range(B)]
+    barred = torch.from_numpy(~c.ok).to(gpu_device)
+    c.logits[barred] = torch.tensor([float("nan"), float("inf"), -1.0], device=gpu_device).to(dtype)[torch.arange(int(barred.sum()), device=gpu_device) % 3]
+    got = c.run()
+    finite = c.logits.clone()
+    finite[barred] = -1.0
+    c.logits = finite
+    assert torch.equal(c.run(), got)
+    c.check(got)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,n,V", [(1, 2, 1500), (1, 2, 20_000), (70, 4, 5003)])
+def test_tokens_done_apart_side_by_side(gpu_device, B, n, V, dtype):
+    """Many biased tokens of one block, in its two halves, at its edges, at the end of a vocabulary, some of them barred, said, on a path."""
+    c = Call(B, n, V, dtype, 41, bias=300)
+    c.bt[:, :280] = c.rng.permuted(np.tile(np.arange(500, 780), (B, 1)), axis=1)
+    c.bt[:, 280:290] = np.arange(V - 10, V)
+    c.bt[:, 290:] = c.bt[:, :10]
+    c.tokens[:, 0], c.tokens[:, 1] = 511, V - 1
+    c.temp[:] = [(1.3, 0.0, 0.8)[b % 3] for b in range(B)]
+    c.check(c.run())
