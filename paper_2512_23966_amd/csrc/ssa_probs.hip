@@ -24,7 +24,7 @@ namespace {
 // tokens in a row it would be 16 bytes of every 32: 670 MB in and out 179 us, with halves 147.)
 constexpr int kUnit = 8, kHalf = 256, kBlock = 2 * kHalf;
 __device__ __forceinline__ constexpr int token_of(int x, int i) { return x + (i & 3) + (i >> 2) * kHalf; }     // token i of a lane whose first is x
-constexpr int kThreads = 256, kStep = kUnit * kThreads, kRowThreads = 512;
+constexpr int kThreads = 256, kStep = kUnit * kThreads;
 constexpr int kMostSlice = 131072;               // tokens of a slice (a bit each in LDS)
 constexpr int kMostSpecial = kTreeNodes + kMostBias;
 
@@ -197,8 +197,12 @@ struct Special {
     int32_t first[kMostSlice / kBlock], next[kMostSpecial];
 };
 
-// One row's slice [x0, x1): the tokens that are done apart, and what the pass over the others needs. PLAIN: there are no such tokens, no record and no grammar.
-template <typename E, int THREADS, bool PLAIN>
+// kPlain: no tokens that are done apart, no record and no grammar; kNoRecord: no record. (Kernels of their own: a wait for what a wave has asked for counts the loads behind it,
+// and with loads that may be there or not it is for all of them.)
+constexpr int kPlain = 0, kNoRecord = 1, kRecord = 2;
+
+// One row's slice [x0, x1): the tokens that are done apart, and what the pass over the others needs.
+template <typename E, int THREADS, int KIND>
 struct Slice {
     const ProbsParams &p;
     const E *row;
@@ -220,7 +224,7 @@ struct Slice {
         allowed = p.allowed ? (const uint8_t *)(p.allowed + row_index * p.words) : nullptr;
         x0 = slice * p.slice_len;
         x1 = x0 + p.slice_len < p.V ? x0 + p.slice_len : p.V;
-        if constexpr (PLAIN) {
+        if constexpr (KIND == kPlain) {
             entries = 0;
             return;
         }
@@ -282,7 +286,7 @@ struct Slice {
     {
         constexpr int W = Raw<E>::kWords;
         raw.ok = ok_of(x, whole);
-        if (!PLAIN && !__any(raw.ok != 0)) return;                   // (none of 512 tokens is allowed)
+        if (KIND != kPlain && whole && !__any(raw.ok != 0)) x = 4 * (threadIdx.x & 63) + x0;         // (none of 512 tokens is allowed: something that a cache has)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;
@@ -297,7 +301,7 @@ struct Slice {
             } else {
                 __builtin_memcpy(raw.l + h * W, row + xh, 4 * sizeof(E));      // (rows of odd vocabularies are aligned to their elements only)
             }
-            if (!PLAIN && seen) {
+            if constexpr (KIND == kRecord) {
                 const u32x2 z = *(const u32x2 *)(seen + xh);
                 raw.z[2 * h] = z[0];
                 raw.z[2 * h + 1] = z[1];
@@ -313,7 +317,7 @@ struct Slice {
             const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;
             if (n <= 0) continue;
             uint32_t ok = 15u;
-            if (!PLAIN && (entries || allowed)) ok = ~((uint32_t)((const uint8_t *)bits)[(xh - x0) >> 3] >> (xh & 4)) & 15u;
+            if (KIND != kPlain && (entries || allowed)) ok = ~((uint32_t)((const uint8_t *)bits)[(xh - x0) >> 3] >> (xh & 4)) & 15u;
             if (!whole && n < 4) ok &= (1u << n) - 1;
             all |= ok << (4 * h);
         }
@@ -323,7 +327,7 @@ struct Slice {
     template <bool SOFT>
     __device__ __forceinline__ void changed(int x, bool whole, const Raw<E> &raw, float (&l)[kUnit]) const
     {
-        if (!PLAIN && !__any(raw.ok != 0)) {
+        if (KIND != kPlain && !__any(raw.ok != 0)) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) l[i] = LOZA_NEG_INF;
             return;
@@ -332,7 +336,7 @@ struct Slice {
         for (int i = 0; i < kUnit; ++i) l[i] = raw.logit(i);
         // (branches of whole waves: a branch of lanes has the compiler keep a copy of everything)
         bool again = false;
-        if (!PLAIN && __any((raw.z[0] | raw.z[1] | raw.z[2] | raw.z[3]) != 0)) {
+        if (KIND == kRecord && __any((raw.z[0] | raw.z[1] | raw.z[2] | raw.z[3]) != 0)) {
             auto z = [&](int i) { return raw.record(i); };
             if constexpr (SOFT) change.soft(l, z);
             else change.quickly(l, z);
@@ -343,7 +347,7 @@ struct Slice {
 #pragma unroll
         for (int i = 0; i < kUnit; i += 2) nans |= __builtin_amdgcn_ballot_w64(__builtin_isunordered(l[i], l[i + 1]));
         if (again || nans) {
-            if (PLAIN || SOFT) {
+            if (KIND == kPlain || SOFT) {
 #pragma unroll
                 for (int i = 0; i < kUnit; ++i) l[i] = settle(l[i]);
             } else {
@@ -361,7 +365,7 @@ struct Slice {
                 }
             }
         }
-        if ((!PLAIN || !whole) && __any(raw.ok != 0xffu)) {
+        if ((KIND != kPlain || !whole) && __any(raw.ok != 0xffu)) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) {
                 const uint32_t keep = (uint32_t)((int32_t)(raw.ok << (31 - i)) >> 31), y = __builtin_bit_cast(uint32_t, l[i]);
@@ -369,25 +373,32 @@ struct Slice {
             }
         }
     }
-    // Calls f(x, raw, whole) for this wave's blocks of 512 tokens, kAhead at a time so that their loads are under way together
+    // Calls f(x, raw, whole) for this wave's blocks of 512 tokens; the next one's loads are under way meanwhile
     template <typename F>
     __device__ __forceinline__ void units(F f) const
     {
-        constexpr int kAhead = sizeof(E) == 2 ? 2 : 1, step = THREADS * kUnit;
+        constexpr int step = THREADS * kUnit;
         const int lane4 = 4 * (threadIdx.x & 63);
         int at = x0 + (int)(threadIdx.x >> 6) * kBlock;              // the block's first token
-        for (; at + (kAhead - 1) * step + kBlock <= x1; at += kAhead * step) {
-            Raw<E> raw[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) load(at + k * step + lane4, true, raw[k]);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) f(at + k * step + lane4, raw[k], true);
+        Raw<E> raw[2];
+        auto there = [&](int y) { return y + kBlock <= x1; };
+        if (there(at)) {
+            load(at + lane4, true, raw[0]);
+            for (;;) {
+                // (behind the last one the same again: always as many loads)
+                load((there(at + step) ? at + step : at) + lane4, true, raw[1]);
+                f(at + lane4, raw[0], true);
+                at += step;
+                if (!there(at)) break;
+                load((there(at + step) ? at + step : at) + lane4, true, raw[0]);
+                f(at + lane4, raw[1], true);
+                at += step;
+                if (!there(at)) break;
+            }
         }
         for (; at < x1; at += step) {
-            Raw<E> raw;
-            const bool whole = at + kBlock <= x1;
-            load(at + lane4, whole, raw);
-            f(at + lane4, raw, whole);
+            load(at + lane4, false, raw[0]);
+            f(at + lane4, raw[0], false);
         }
     }
     // An entry of a list, the same for the whole wave
@@ -447,8 +458,8 @@ __device__ __forceinline__ Stat workgroup_stat(Stat a, const Weight &w, Stat *ld
 constexpr Stat kNoStat = {LOZA_NEG_INF, 0.f, 0x7fffffff, 0};
 
 // Stat of this thread's share of a slice
-template <bool SOFT, typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, PLAIN> &s, const Weight &w)
+template <bool SOFT, typename E, int THREADS, int KIND>
+__device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, KIND> &s, const Weight &w)
 {
     Stat a = kNoStat;
     s.units([&](int x, const Raw<E> &raw, bool whole) {
@@ -476,7 +487,7 @@ __device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, PLAIN> &s,
             }
         }
     });
-    if constexpr (!PLAIN)
+    if constexpr (KIND != kPlain)
         for (int i = threadIdx.x; i < s.entries; i += THREADS)
             if (s.lds.tok[i] >= 0) merge(a, s.lds.val[i], 1.f, s.lds.tok[i], w);
     return a;
@@ -503,8 +514,8 @@ __device__ __forceinline__ void store_unit(float *out, int x, int V, bool whole,
 }
 
 // The probabilities of a slice of a row that is not greedy, given the row's Stat
-template <bool NT, typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ void write_soft(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, const Weight &w)
+template <bool NT, typename E, int THREADS, int KIND>
+__device__ __forceinline__ void write_soft(const Slice<E, THREADS, KIND> &s, float *out, const Stat &a, const Weight &w)
 {
     const float inv = a.m == LOZA_NEG_INF ? 0.f : 1.f / a.s;
     const bool infinite = a.m == __builtin_inff() || a.m == LOZA_NEG_INF;       // (nothing weighs: 0 for all)
@@ -519,7 +530,7 @@ __device__ __forceinline__ void write_soft(const Slice<E, THREADS, PLAIN> &s, fl
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) l[i] = w(l[i] - a.m) * inv;
         }
-        if (!PLAIN && s.entries) {
+        if (KIND != kPlain && s.entries) {
             // those done apart, into what is stored (single words behind it took 10 us of 170 for 64 of them in each of 853 rows)
             for (int e = s.list(s.lds.first, (x - s.x0) / kBlock); e >= 0; e = s.list(s.lds.next, e)) {
                 const int at = s.lds.tok[e] - x;
@@ -533,8 +544,8 @@ __device__ __forceinline__ void write_soft(const Slice<E, THREADS, PLAIN> &s, fl
 }
 
 // ... of a greedy one: nothing is read again
-template <bool NT, typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ void write_greedy(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a)
+template <bool NT, typename E, int THREADS, int KIND>
+__device__ __forceinline__ void write_greedy(const Slice<E, THREADS, KIND> &s, float *out, const Stat &a)
 {
     for (int at = s.x0 + (int)(threadIdx.x >> 6) * kBlock; at < s.x1; at += THREADS * kUnit) {
         const int x = at + 4 * (threadIdx.x & 63);
@@ -545,13 +556,13 @@ __device__ __forceinline__ void write_greedy(const Slice<E, THREADS, PLAIN> &s, 
     }
 }
 
-template <typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS, PLAIN> &s, float t, const Weight &w)
+template <typename E, int THREADS, int KIND>
+__device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS, KIND> &s, float t, const Weight &w)
 {
     return t > 0.f ? thread_stat_t<true>(s, w) : thread_stat_t<false>(s, w);
 }
-template <bool NT, typename E, int THREADS, bool PLAIN>
-__device__ __forceinline__ void write_probs(const Slice<E, THREADS, PLAIN> &s, float *out, const Stat &a, float t, const Weight &w)
+template <bool NT, typename E, int THREADS, int KIND>
+__device__ __forceinline__ void write_probs(const Slice<E, THREADS, KIND> &s, float *out, const Stat &a, float t, const Weight &w)
 {
     if (t > 0.f) write_soft<NT>(s, out, a, w);
     else write_greedy<NT>(s, out, a);
@@ -563,7 +574,7 @@ __device__ __forceinline__ bool row_there(const ProbsParams &p, int64_t row)
     return p.tree_lens == nullptr || (int)(row % p.n) < p.tree_lens[row / p.n];
 }
 
-template <typename E, bool PLAIN>
+template <typename E, int KIND>
 __global__ __launch_bounds__(kThreads) void token_stats_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
@@ -571,14 +582,14 @@ __global__ __launch_bounds__(kThreads) void token_stats_kernel(const ProbsParams
     __shared__ Stat s_stat[kThreads / 64];
     const int64_t row = blockIdx.x / p.slices;
     if (!row_there(p, row)) return;
-    const Slice<E, kThreads, PLAIN> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
+    const Slice<E, kThreads, KIND> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     const Stat a = workgroup_stat<kThreads>(thread_stat(s, t, w), w, s_stat);
     if (threadIdx.x == 0) ((Stat *)p.stats)[blockIdx.x] = a;
 }
 
-template <typename E, bool PLAIN, bool NT>
+template <typename E, int KIND, bool NT>
 __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
@@ -586,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams
     __shared__ Stat s_stat[kThreads / 64];
     const int64_t row = blockIdx.x / p.slices;
     if (!row_there(p, row)) return;
-    const Slice<E, kThreads, PLAIN> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
+    const Slice<E, kThreads, KIND> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     Stat a = kNoStat;
@@ -599,18 +610,18 @@ __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams
 }
 
 // A workgroup a row, in one launch: the row is read again for the probabilities, from a cache that holds what is under way.
-template <typename E, bool PLAIN, bool NT>
-__global__ __launch_bounds__(kRowThreads) void token_row_kernel(const ProbsParams p)
+template <typename E, int THREADS, int KIND, bool NT>
+__global__ __launch_bounds__(THREADS) void token_row_kernel(const ProbsParams p)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t s_bits[];
     __shared__ Special s_special;
-    __shared__ Stat s_stat[kRowThreads / 64];
+    __shared__ Stat s_stat[THREADS / 64];
     const int64_t row = blockIdx.x;
     if (!row_there(p, row)) return;
-    const Slice<E, kRowThreads, PLAIN> s(p, row, 0, s_special, s_bits);
+    const Slice<E, THREADS, KIND> s(p, row, 0, s_special, s_bits);
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
-    const Stat a = workgroup_stat<kRowThreads>(thread_stat(s, t, w), w, s_stat);
+    const Stat a = workgroup_stat<THREADS>(thread_stat(s, t, w), w, s_stat);
     write_probs<NT>(s, p.probs + row * p.V, a, t, w);
 }
 
@@ -729,8 +740,8 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
 }  // namespace
 
 // A workgroup a row where there are many rows or they are short (up to 12,288 tokens, a row a 256 tokens, 256 rows), else slices: 2,048 workgroups in all as far as
-// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 10 and 13, 512 rows 19 and 28; 32,003,
-// 1 row 20 and 13, 64 rows 23 and 17, 128 rows 26 and 30; 131,072, 1 row 51 and 13, 192 rows 72 and 61, 256 rows 74 and 75, 512 rows 104 and 117.
+// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 10 and 12, 512 rows 18 and 24; 32,003,
+// 1 row 18 and 12, 64 rows 22 and 17, 128 rows 24 and 23; 131,072, 1 row 39 and 12, 128 rows 49 and 41, 256 rows 62 and 66, 512 rows 90 and 101.
 void probs_plan(ProbsParams &p)
 {
     const int64_t rows = (int64_t)p.B * p.n;
@@ -743,33 +754,40 @@ void probs_plan(ProbsParams &p)
     p.words = (int)(((int64_t)p.V + 31) / 32);
 }
 
-template <typename E, bool PLAIN, bool NT>
+template <typename E, int KIND, bool NT>
 static hipError_t launch_probs_t(const ProbsParams &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)((int64_t)p.B * p.n * p.slices));
     const size_t lds = p.masks || p.n_bias || p.allowed ? (size_t)(p.slice_len < p.V ? p.slice_len : p.V + 31) / 32 * 4 : 0;
     if (p.slices == 1) {
-        hipLaunchKernelGGL((token_row_kernel<E, PLAIN, NT>), grid, dim3(kRowThreads), lds, stream, p);
+        // Threads of a row, us with 256, 512 and 1,024 of them: 2,048 rows of 700 tokens 19, 29, 45, of 8,000 36, 45, 57, of 16,000 59, 62, 76; 256 rows of 8,000 15, 13, 13;
+        // 512 rows of 32,003 38, 33, 33; 256 rows of 131,072 102, 66, 62, 1,024 rows 235, 226, 212.
+        // (65,535 trees of 64 rows of 1,024 threads are as many as a launch takes)
+        static_assert(65535LL * kTreeNodes * 1024 <= 0xffffffffLL);
+        const int threads = p.V > 65536 ? 1024 : grid.x >= 768 && p.V <= 16384 ? 256 : 512;
+        if (threads == 1024) hipLaunchKernelGGL((token_row_kernel<E, 1024, KIND, NT>), grid, dim3(1024), lds, stream, p);
+        else if (threads == 512) hipLaunchKernelGGL((token_row_kernel<E, 512, KIND, NT>), grid, dim3(512), lds, stream, p);
+        else hipLaunchKernelGGL((token_row_kernel<E, 256, KIND, NT>), grid, dim3(256), lds, stream, p);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((token_stats_kernel<E, PLAIN>), grid, dim3(kThreads), lds, stream, p);
+    hipLaunchKernelGGL((token_stats_kernel<E, KIND>), grid, dim3(kThreads), lds, stream, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL((token_probs_kernel<E, PLAIN, NT>), grid, dim3(kThreads), lds, stream, p);
+    hipLaunchKernelGGL((token_probs_kernel<E, KIND, NT>), grid, dim3(kThreads), lds, stream, p);
     return hipGetLastError();
 }
 
-template <typename E, bool PLAIN>
+template <typename E, int KIND>
 static hipError_t launch_probs_p(const ProbsParams &p, hipStream_t stream)
 {
     // Results that no cache holds are stored past the caches, which keep the logits for their second reading (1,024 rows of 131,072 bf16 logits 244 -> 162 us)
-    return (int64_t)p.B * p.n * p.V * 4 >= 128 << 20 ? launch_probs_t<E, PLAIN, true>(p, stream) : launch_probs_t<E, PLAIN, false>(p, stream);
+    return (int64_t)p.B * p.n * p.V * 4 >= 128 << 20 ? launch_probs_t<E, KIND, true>(p, stream) : launch_probs_t<E, KIND, false>(p, stream);
 }
 
 template <typename E>
 static hipError_t launch_probs_e(const ProbsParams &p, hipStream_t stream)
 {
-    const bool plain = !p.masks && !p.n_bias && !p.allowed && !p.seen;
-    return plain ? launch_probs_p<E, true>(p, stream) : launch_probs_p<E, false>(p, stream);
+    if (p.seen) return launch_probs_p<E, kRecord>(p, stream);
+    return p.masks || p.n_bias || p.allowed ? launch_probs_p<E, kNoRecord>(p, stream) : launch_probs_p<E, kPlain>(p, stream);
 }
 
 hipError_t launch_token_probs(const ProbsParams &p, int elem_bytes, hipStream_t stream)

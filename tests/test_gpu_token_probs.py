@@ -346,3 +346,15 @@ def test_tokens_done_apart_side_by_side(gpu_device, B, n, V, dtype):
     c.tokens[:, 0], c.tokens[:, 1] = 511, V - 1
     c.temp[:] = [(1.3, 0.0, 0.8)[b % 3] for b in range(B)]
     c.check(c.run())
+
+
+@pytest.mark.parametrize("parts", ["all of it", "no record", "nothing"])
+@pytest.mark.parametrize("B,n,V", [(256, 1, 66_001), (4, 64, 131_072), (4, 64, 65_536), (800, 1, 16_384), (12, 64, 16_385), (800, 1, 1025), (400, 2, 513), (800, 1, 511)])
+def test_rows_of_each_number_of_threads(gpu_device, B, n, V, parts):
+    for dtype in (BF, F32):
+        c = Call(B, n, V, dtype, V, bias=9)
+        if parts != "all of it":
+            c.seen = None
+        if parts == "nothing":
+            c.masks = c.tokens = c.bt = c.bv = c.ok = None
+        c.check(c.run(), (0, n // 2, n - 1) if B < 100 else None)
