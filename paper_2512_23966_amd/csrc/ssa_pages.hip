@@ -28,6 +28,31 @@ __device__ __forceinline__ int64_t valid_count(const int32_t *count, int64_t num
     return c < 0 ? 0 : c < num_free ? c : num_free;
 }
 
+// Numbers before this thread's in a workgroup of 1,024 (each 0 .. 4)
+__device__ __forceinline__ int scan_before(int x, int32_t *lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += up;
+    }
+    if (lane == 63) lds[wave] = sum;
+    __syncthreads();
+    int before = sum - x;
+    for (int i = 0; i < wave; ++i) before += lds[i];
+    __syncthreads();
+    return before;
+}
+
+// Small pools are done by one workgroup, with a number a page in LDS: one launch in the place of two (forks), three (pages given back) or four (compaction), which are also 3 us
+// each of the host's time. us in a graph, several launches and one: 1,000 pages and 12 requests 5.4 and 4.0, 8.6 and 4.4, 13 and 4.0; 8,000 pages, 64 requests of 128 entries 5.7
+// and 5.4, 10.3 and 8.6, 19 and 9; 256 requests of 64 6.0 and 7.1, 9.7 and 9.8, 19 and 11; 1,000 requests of 16 8 and 13, 10 and 16, 18 and 11.
+constexpr int kSmallPages = 8192, kSmallRequests = 128, kSmallThreads = 1024;
+constexpr int64_t kSmallRow = 512, kSmallTable = 32768;              // entries of a request; of all for a compaction
+bool small(int64_t num_pages, int64_t B, int64_t max_pages) { return num_pages <= kSmallPages && B <= kSmallRequests && max_pages <= kSmallRow; }
+
 // ---- forks ---------------------------------------------------------------------------------------------
 
 __global__ __launch_bounds__(256) void copy_ints_kernel(const int32_t *__restrict__ from, int32_t *__restrict__ to, int64_t n)
@@ -51,6 +76,25 @@ __device__ __forceinline__ Fork fork_of(const ForkParams &p, int b)
     if (f.rows < 0 || f.rows > (int64_t)p.max_pages << p.page_shift) f.fits = false;
     f.need = f.fits && (f.rows & (((int64_t)1 << p.page_shift) - 1)) != 0;
     return f;
+}
+
+// Writes what becomes of request b; `before`: pages that the requests before it need
+__device__ __forceinline__ void fork_made(const ForkParams &p, int b, const Fork &f, bool ok, int64_t full, int64_t first, int64_t before, int64_t count)
+{
+    const bool started = ok && f.need;
+    int source = -1, target = -1;
+    if (started) {
+        source = p.block_table[(int64_t)f.source * p.max_pages + full];
+        target = p.free_pages[count - 1 - before];
+        p.block_table[(int64_t)b * p.max_pages + full] = target;
+    }
+    p.forked[b] = ok;
+    p.cache_lens_after[b] = ok ? (int32_t)f.rows : p.cache_lens[b];
+    p.held_after[b] = ok ? (int32_t)(full + f.need) : p.held[b];
+    if (p.trimmed) p.trimmed_after[b] = ok ? (int32_t)first : p.trimmed[b];
+    p.copy_from[b] = source;
+    p.copy_to[b] = target;
+    p.copy_rows[b] = started ? (int32_t)(f.rows & (((int64_t)1 << p.page_shift) - 1)) : 0;
 }
 
 // A workgroup a request. Pages are dealt out in the order of the requests: each adds up what those before its own need.
@@ -82,21 +126,42 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(const ForkParams p)
         to[i] = page;
         if ((i < p.sink_pages || i >= first) && page >= 0 && page < p.num_pages) atomicAdd(&p.shared_after[page], 1);
     }
-    if (tid != 0) return;
-    const bool started = ok && f.need;
-    int source = -1, target = -1;
-    if (started) {
-        source = from[full];
-        target = p.free_pages[count - 1 - before];
-        to[full] = target;
+    if (tid == 0) fork_made(p, b, f, ok, full, first, before, count);
+}
+
+__global__ __launch_bounds__(kSmallThreads) void pages_fork_small_kernel(const ForkParams p)
+{
+    __shared__ int32_t s_shared[kSmallPages], s_source[kSmallRequests], s_full[kSmallRequests], s_first[kSmallRequests], s_scan[16];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, pages = (int)p.num_pages;
+    const int64_t count = valid_count(p.free_count, p.num_free);
+    Fork f{-1, 0, false, 0};
+    if (tid < p.B) f = fork_of(p, tid);
+    for (int i = tid; i < pages; i += kSmallThreads) s_shared[i] = p.shared[i];
+    const int before = scan_before(f.need, s_scan);
+    const bool ok = f.fits && (f.need == 0 || before < count);
+    const int full = ok ? (int)(f.rows >> p.page_shift) : 0, first = p.trimmed && ok ? p.trimmed[f.source] : 0;
+    if (tid < p.B) {
+        s_source[tid] = f.source;
+        s_full[tid] = full;
+        s_first[tid] = first;
+        fork_made(p, tid, f, ok, full, first, before, count);
     }
-    p.forked[b] = ok;
-    p.cache_lens_after[b] = ok ? (int32_t)f.rows : p.cache_lens[b];
-    p.held_after[b] = ok ? (int32_t)(full + f.need) : p.held[b];
-    if (p.trimmed) p.trimmed_after[b] = ok ? (int32_t)first : p.trimmed[b];
-    p.copy_from[b] = source;
-    p.copy_to[b] = target;
-    p.copy_rows[b] = started ? (int32_t)(f.rows & (((int64_t)1 << p.page_shift) - 1)) : 0;
+    if (tid == kSmallThreads - 1) {
+        const int64_t all = before + f.need;
+        p.free_left[0] = (int32_t)(count - (all < count ? all : count));
+    }
+    __syncthreads();
+    for (int b = wave; b < p.B; b += kSmallThreads / 64) {           // a wave a request
+        const int32_t *from = p.block_table + (int64_t)s_source[b] * p.max_pages;
+        int32_t *to = p.block_table + (int64_t)b * p.max_pages;
+        for (int i = lane; i < s_full[b]; i += 64) {
+            const int page = from[i];
+            to[i] = page;
+            if ((i < p.sink_pages || i >= s_first[b]) && page >= 0 && page < pages) atomicAdd(&s_shared[page], 1);
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < pages; i += kSmallThreads) p.shared_after[i] = s_shared[i];
 }
 
 // ---- copies ---------------------------------------------------------------------------------------------
@@ -150,38 +215,47 @@ __global__ __launch_bounds__(256) void free_start_kernel(const FreeParams p)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p.freed[i] = 0;
 }
 
-__global__ __launch_bounds__(256) void free_mark_kernel(const FreeParams p)
+// Entries [0, sink) and [first, upto) of request b's row are given up; `write`: and what the request has then is written
+struct GivenUp {
+    int64_t sink, first, upto;
+};
+__device__ __forceinline__ GivenUp given_up(const FreeParams &p, int b, bool write)
 {
-    const int b = blockIdx.x;
     const int64_t size = (int64_t)1 << p.page_shift, len = p.cache_lens[b], held = p.held[b];
     const int trimmed = p.trimmed ? p.trimmed[b] : 0;
     const bool fits = len >= 0 && len <= (int64_t)p.max_pages * size && held >= 0 && held <= p.max_pages;
     const bool ends = fits && p.ending && p.ending[b] != 0;
     const int64_t used = (len + size - 1) >> p.page_shift, have = held > used ? held : used;
-    int64_t first = trimmed > p.sink_pages ? trimmed : p.sink_pages;     // entries [0, sink_pages) and [first, have) are the request's
-    int64_t upto = first;                                                // entries [first, upto) are given up, and the sink's where the request ends
+    const int64_t first = trimmed > p.sink_pages ? trimmed : p.sink_pages;      // entries [0, sink_pages) and [first, have) are the request's
+    int64_t upto = first;
     if (ends) {
         upto = have;
     } else if (fits && p.trimmed) {
         const int64_t seen = (int64_t)window_begin_of((int)len, p.window, p.block) >> p.page_shift;
         upto = seen > first ? seen : first;
     }
-    if (blockIdx.y == 0 && threadIdx.x == 0) {
+    if (write) {
         p.cache_lens_after[b] = ends ? 0 : (int32_t)len;
         p.held_after[b] = ends ? 0 : (int32_t)held;
         if (p.trimmed) p.trimmed_after[b] = ends ? 0 : upto > p.sink_pages ? (int32_t)(upto > trimmed ? upto : trimmed) : trimmed;
     }
-    if (!fits) return;
+    if (!fits) return GivenUp{0, 0, 0};
+    return GivenUp{!ends ? 0 : p.sink_pages < have ? p.sink_pages : have, first, upto < have ? upto : have};
+}
+
+__global__ __launch_bounds__(256) void free_mark_kernel(const FreeParams p)
+{
+    const int b = blockIdx.x;
+    const GivenUp g = given_up(p, b, blockIdx.y == 0 && threadIdx.x == 0);
     const int32_t *table = p.block_table + (int64_t)b * p.max_pages;
-    const int64_t sink = ends ? (p.sink_pages < have ? p.sink_pages : have) : 0;
     const int64_t step = (int64_t)gridDim.y * 256, me = (int64_t)blockIdx.y * 256 + threadIdx.x;
     auto give = [&](int64_t i) {
         const int page = table[i];
         if (page < 0 || page >= p.num_pages) return;
         if (atomicSub(&p.left[page], 1) == 0) atomicOr(&p.freed[page >> 5], 1u << (page & 31));
     };
-    for (int64_t i = me; i < sink; i += step) give(i);
-    for (int64_t i = first + me; i < upto && i < have; i += step) give(i);
+    for (int64_t i = me; i < g.sink; i += step) give(i);
+    for (int64_t i = g.first + me; i < g.upto; i += step) give(i);
 }
 
 // How many of the bits below `limit` are set, by a workgroup of 1,024
@@ -209,24 +283,6 @@ __device__ __forceinline__ int64_t bits_below(const uint32_t *bits, int64_t limi
     return sum;
 }
 
-// Numbers before this thread's in a workgroup of 1,024 (each 0 .. 4)
-__device__ __forceinline__ int scan_before(int x, int32_t *lds)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int sum = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int up = __shfl_up(sum, d, 64);
-        if (lane >= d) sum += up;
-    }
-    if (lane == 63) lds[wave] = sum;
-    __syncthreads();
-    int before = sum - x;
-    for (int i = 0; i < wave; ++i) before += lds[i];
-    __syncthreads();
-    return before;
-}
-
 // A workgroup a group of kPageGroup pages, 4 a thread
 __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
 {
@@ -250,6 +306,46 @@ __global__ __launch_bounds__(1024) void free_append_kernel(const FreeParams p)
             ++at;
         }
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 1023) p.free_after[0] = (int32_t)(at < p.num_free ? at : p.num_free);   // (behind the last one's own)
+}
+
+__global__ __launch_bounds__(kSmallThreads) void pages_free_small_kernel(const FreeParams p)
+{
+    __shared__ int32_t s_left[kSmallPages], s_scan[16];
+    __shared__ GivenUp s_given[kSmallRequests];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, pages = (int)p.num_pages;
+    const int64_t count = valid_count(p.free_count, p.num_free);
+    if (tid < p.B) s_given[tid] = given_up(p, tid, true);
+    for (int i = tid; i < pages; i += kSmallThreads) s_left[i] = p.shared ? p.shared[i] : 0;
+    __syncthreads();
+    for (int b = wave; b < p.B; b += kSmallThreads / 64) {           // a wave a request
+        const GivenUp g = s_given[b];
+        const int32_t *table = p.block_table + (int64_t)b * p.max_pages;
+        auto give = [&](int64_t i) {
+            const int page = table[i];
+            if (page >= 0 && page < pages) atomicSub(&s_left[page], 1);
+        };
+        for (int64_t i = lane; i < g.sink; i += 64) give(i);
+        for (int64_t i = g.first + lane; i < g.upto; i += 64) give(i);
+    }
+    __syncthreads();
+    // 8 pages a thread, in order
+    constexpr int kEach = kSmallPages / kSmallThreads;
+    int left[kEach], mine = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int page = tid * kEach + k;
+        left[k] = page < pages ? s_left[page] : 0;
+        mine += left[k] < 0;
+        if (p.shared && page < pages) p.shared_after[page] = left[k] < 0 ? 0 : left[k];
+    }
+    int64_t at = count + scan_before(mine, s_scan);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+        if (left[k] < 0) {
+            if (at < p.num_free) p.free_pages[at] = tid * kEach + k;
+            ++at;
+        }
+    if (tid == kSmallThreads - 1) p.free_after[0] = (int32_t)(at < p.num_free ? at : p.num_free);
 }
 
 // ---- the pool tidied ------------------------------------------------------------------------------------
@@ -319,6 +415,55 @@ __global__ __launch_bounds__(256) void compact_rename_kernel(const CompactParams
         p.shared_after[i] = i >= used ? 0 : p.shared[is_free(i) ? p.copy_from[p.place[i]] : i];
 }
 
+__global__ __launch_bounds__(kSmallThreads) void pages_compact_small_kernel(const CompactParams p)
+{
+    constexpr int kWords = kSmallPages / 32;
+    __shared__ uint32_t s_bits[kWords];                              // free pages
+    __shared__ int32_t s_before[kWords], s_scan[16], s_all;          // how many of them are in the words before
+    __shared__ uint16_t s_from[kSmallPages / 2], s_to[kSmallPages / 2];
+    const int tid = threadIdx.x, pages = (int)p.num_pages;
+    const int64_t count = valid_count(p.free_count, p.num_free);
+    if (tid < kWords) s_bits[tid] = 0;
+    __syncthreads();
+    for (int64_t i = tid; i < count; i += kSmallThreads) {
+        const int page = p.free_pages[i];
+        if (page >= 0 && page < pages) atomicOr(&s_bits[page >> 5], 1u << (page & 31));
+    }
+    __syncthreads();
+    const int mine = tid < kWords ? __popc(s_bits[tid]) : 0, sum = scan_before(mine, s_scan);
+    if (tid < kWords) s_before[tid] = sum;
+    if (tid == kWords - 1) s_all = sum + mine;
+    __syncthreads();
+    auto is_free = [&](int page) { return s_bits[page >> 5] >> (page & 31) & 1u; };
+    auto frees = [&](int page) { return s_before[page >> 5] + __popc(s_bits[page >> 5] & ((1u << (page & 31)) - 1)); };     // of the pages below
+    const int all = s_all, used = pages - all, holes = all > 0 ? frees(used) : 0, most = pages / 2;
+    for (int page = tid; page < pages; page += kSmallThreads) {
+        const bool is = is_free(page);
+        if (is && page < used) {
+            s_to[frees(page)] = (uint16_t)page;
+            p.copy_to[frees(page)] = page;
+        } else if (!is && page >= used) {
+            const int i = page - frees(page) - (used - holes);
+            s_from[i] = (uint16_t)page;
+            p.copy_from[i] = page;
+        }
+        if (page >= holes && page < most) p.copy_from[page] = p.copy_to[page] = -1;
+    }
+    for (int64_t i = tid; i < p.num_free; i += kSmallThreads) p.free_pages_after[i] = i < all ? (int32_t)(pages - 1 - i) : -1;
+    if (tid == 0) {
+        p.free_after[0] = all;
+        p.n_copies[0] = holes;
+    }
+    __syncthreads();
+    const int entries = p.B * p.max_pages;
+    for (int i = tid; i < entries; i += kSmallThreads) {
+        const int page = p.block_table[i];
+        p.table_after[i] = page >= used && page < pages && !is_free(page) ? s_to[page - frees(page) - (used - holes)] : page;
+    }
+    if (p.shared == nullptr) return;
+    for (int i = tid; i < pages; i += kSmallThreads) p.shared_after[i] = i >= used ? 0 : p.shared[is_free(i) ? s_from[frees(i)] : i];
+}
+
 unsigned blocks_for(int64_t n, int threads, int64_t most)
 {
     const int64_t b = (n + threads - 1) / threads;
@@ -329,6 +474,10 @@ unsigned blocks_for(int64_t n, int threads, int64_t most)
 
 hipError_t launch_pages_fork(const ForkParams &p, hipStream_t stream)
 {
+    if (small(p.num_pages, p.B, p.max_pages)) {
+        hipLaunchKernelGGL(pages_fork_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(copy_ints_kernel, dim3(blocks_for(p.num_pages, 256, 1024)), dim3(256), 0, stream, p.shared, p.shared_after, p.num_pages);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)p.B), dim3(256), 0, stream, p);
@@ -348,6 +497,10 @@ hipError_t launch_pages_copy(const CopyParams &p, hipStream_t stream)
 
 hipError_t launch_pages_free(const FreeParams &p, hipStream_t stream)
 {
+    if (small(p.num_pages, p.B, p.max_pages)) {
+        hipLaunchKernelGGL(pages_free_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(free_start_kernel, dim3(blocks_for(p.num_pages, 256, 1024)), dim3(256), 0, stream, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(free_mark_kernel, dim3((unsigned)p.B, blocks_for(p.max_pages, 1024, 16)), dim3(256), 0, stream, p);
@@ -358,6 +511,10 @@ hipError_t launch_pages_free(const FreeParams &p, hipStream_t stream)
 
 hipError_t launch_pages_compact(const CompactParams &p, hipStream_t stream)
 {
+    if (p.num_pages <= kSmallPages && p.num_free <= kSmallTable && (int64_t)p.B * p.max_pages <= kSmallTable) {
+        hipLaunchKernelGGL(pages_compact_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(compact_start_kernel, dim3(blocks_for(p.num_pages / 32 + 1, 256, 256)), dim3(256), 0, stream, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(compact_mark_kernel, dim3(blocks_for(p.num_free, 256, 1024)), dim3(256), 0, stream, p);

@@ -173,9 +173,10 @@ def test_copies_beyond_2_32_bytes(gpu_device):
     torch.cuda.empty_cache()
 
 
-def test_calls_are_repeatable_also_in_a_graph(gpu_device):
+@pytest.mark.parametrize("spare", [5, 9000])
+def test_calls_are_repeatable_also_in_a_graph(gpu_device, spare):
     rng = np.random.default_rng(3)
-    p = Pool(rng, 50, 32, 40)
+    p = Pool(rng, 50, 32, 40, spare=spare)
     source = rng.integers(-1, 50, size=50).astype(np.int32)
     i32 = dict(dtype=I32, device=gpu_device)
     ins = {k: _dev(x, gpu_device) for k, x in (("source", source), ("lens", p.lens), ("held", p.held), ("trimmed", p.trimmed), ("free", p.free), ("shared", p.shared), ("table", p.table),
@@ -211,3 +212,29 @@ def test_calls_are_repeatable_also_in_a_graph(gpu_device):
         torch.cuda.synchronize()
         for name in o:
             assert torch.equal(o[name], ref[name]), (k, name)
+
+
+# ---- a pool small enough for one workgroup, and just not -----------------------------------------------------------------
+
+@pytest.mark.parametrize("B,page,most", [(128, 32, 100), (129, 32, 30), (20, 32, 512), (20, 32, 513), (31, 32, 400)])
+def test_forks_and_frees_around_one_workgroup(gpu_device, B, page, most):
+    test_fork(gpu_device, B, page, most)
+    test_free(gpu_device, B, page, most)
+
+
+@pytest.mark.parametrize("pages,B,most,extra", [(8191, 8, 40, 0), (8192, 1, 32_768, 3), (8192, 1, 32_769, 0), (8193, 8, 40, 0), (100, 1000, 33, 0), (50, 3, 20, 32_718), (50, 3, 20, 32_719)])
+def test_compact_around_one_workgroup(gpu_device, pages, B, most, extra):
+    rng = np.random.default_rng(pages + most)
+    perm = rng.permutation(pages).astype(np.int32)
+    for count in (0, 1, pages // 3, pages - 1, pages):
+        free = np.full(pages + extra, 5, dtype=np.int32)
+        free[:count] = perm[:count]
+        table, shared = rng.integers(-2, pages + 2, size=(B, most)).astype(np.int32), rng.integers(0, 4, size=pages).astype(np.int32)
+        i32 = dict(dtype=I32, device=gpu_device)
+        o = {"table": torch.empty(B, most, **i32), "free": torch.full((pages + extra,), -77, **i32), "count": torch.empty(1, **i32), "shared": torch.full((pages,), -77, **i32),
+             "copy_from": torch.full((pages // 2,), -77, **i32), "copy_to": torch.full((pages // 2,), -77, **i32), "copies": torch.empty(1, **i32)}
+        loza.loza_ssa_pages_compact(_dev(table, gpu_device), _dev(free, gpu_device), torch.tensor([count], **i32), _dev(shared, gpu_device), pages, o["table"], o["free"], o["count"],
+                                    o["shared"], o["copy_from"], o["copy_to"], o["copies"])
+        ref = N.pages_compact(table, free, count, shared, pages)
+        for k in ref:
+            assert np.array_equal(o[k].cpu().numpy(), ref[k]), (count, k)
