@@ -289,20 +289,18 @@ struct Slice {
         if (KIND != kPlain && whole && !__any(raw.ok != 0)) x = 4 * (threadIdx.x & 63) + x0;         // (none of 512 tokens is allowed: something that a cache has)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int xh = x + h * kHalf, n = whole ? 4 : p.V - xh;
+            const int xh = x + h * kHalf;
             raw.z[2 * h] = raw.z[2 * h + 1] = 0;
-            if (!whole && n < 4) {
-                E e[4] = {};
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < n) e[i] = row[xh + i];
-                __builtin_memcpy(raw.l + h * W, e, sizeof(e));
-                if (n <= 0) continue;
-            } else {
+            if (whole) {
                 __builtin_memcpy(raw.l + h * W, row + xh, 4 * sizeof(E));      // (rows of odd vocabularies are aligned to their elements only)
+            } else {                                                           // tokens that are not there: the last one again
+                E e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = row[xh + i < p.V ? xh + i : p.V - 1];
+                __builtin_memcpy(raw.l + h * W, e, sizeof(e));
             }
             if constexpr (KIND == kRecord) {
-                const u32x2 z = *(const u32x2 *)(seen + xh);
+                const u32x2 z = *(const u32x2 *)(seen + (whole || xh < p.V ? xh : (p.V - 1) & ~3));
                 raw.z[2 * h] = z[0];
                 raw.z[2 * h + 1] = z[1];
             }
