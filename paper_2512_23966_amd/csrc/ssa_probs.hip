@@ -5,8 +5,8 @@
 //     l' = l / repetition if l > 0, l * repetition otherwise, where it occurred;  l'' = l' - frequency c - presence (c > 0) + bias
 // and no weight where the grammar does not allow it (or l'' is a NaN); p = exp((l'' - max) / T) / sum, or 1 at the first of the largest.
 //
-// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 155 us, 5.2 TB/s); with everything
-// (the same, 853 of the rows alive) 164 us, 137 of them the memory's, the vector ALU the rest: some 30 instructions a token in two passes, half of them for the record. All of it is done
+// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 168 us, 4.8 TB/s); with everything the vector ALU as well,
+// 39 instructions a token in two passes (the same, 853 of the rows alive: 212 us, 150 where a cache has the logits; the memory's part is 136). All of it is done
 // on the way. The tokens of a tree's own nodes and the biased ones are a few hundred of 100,000: the pass over the row leaves
 // them out (a bit each in LDS), and a thread each does them apart, so that the pass looks nothing up.
 #include <hip/hip_runtime.h>
@@ -666,7 +666,8 @@ __global__ __launch_bounds__(256) void count_tokens_kernel(const CountParams p)
 }
 
 // The same for many tokens: a workgroup takes a slice of a request's row, counts in LDS (bit 31: in the prompt) what of all tokens falls into it, and
-// writes the units of 8 that changed. Every slice reads all tokens, out of L2.
+// writes the units of 8 that changed. Every slice reads all tokens, out of L2, four loads of four under way (16 requests of 100,000 tokens 12.7 us, 14.5 with slices of 16,384,
+// 19.5 with a load at a time).
 constexpr int kCountSlice = 8192, kCountThreads = 1024;
 
 __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountParams p)
