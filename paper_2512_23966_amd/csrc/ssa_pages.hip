@@ -211,7 +211,7 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const CopyParams p)
 __global__ __launch_bounds__(256) void free_start_kernel(const FreeParams p)
 {
     const int64_t words = (p.num_pages + 31) / 32;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.num_pages; i += (int64_t)gridDim.x * 256) p.left[i] = p.shared ? p.shared[i] : 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.num_pages; i += (int64_t)gridDim.x * 256) p.left[i] = p.shared && p.shared[i] > 0 ? p.shared[i] : 0;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p.freed[i] = 0;
 }
 
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kSmallThreads) void pages_free_small_kernel(const F
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, pages = (int)p.num_pages;
     const int64_t count = valid_count(p.free_count, p.num_free);
     if (tid < p.B) s_given[tid] = given_up(p, tid, true);
-    for (int i = tid; i < pages; i += kSmallThreads) s_left[i] = p.shared ? p.shared[i] : 0;
+    for (int i = tid; i < pages; i += kSmallThreads) s_left[i] = p.shared && p.shared[i] > 0 ? p.shared[i] : 0;
     __syncthreads();
     for (int b = wave; b < p.B; b += kSmallThreads / 64) {           // a wave a request
         const GivenUp g = s_given[b];

@@ -25,7 +25,7 @@ namespace {
 constexpr int kUnit = 8, kHalf = 256, kBlock = 2 * kHalf;
 __device__ __forceinline__ constexpr int token_of(int x, int i) { return x + (i & 3) + (i >> 2) * kHalf; }     // token i of a lane whose first is x
 constexpr int kThreads = 256, kStep = kUnit * kThreads;
-constexpr int kMostSlice = 131072;               // tokens of a slice (a bit each in LDS)
+constexpr int kMostSlice = 262144;               // tokens of a slice (a bit each in LDS; 768 rows of 200,064, us: 263, with two slices each 311)
 constexpr int kMostSpecial = kTreeNodes + kMostBias;
 
 // What a row's logits are changed by. Where the largest is asked for (greedy rows) each operation is rounded by itself, as a plain program does them: a token

@@ -358,3 +358,23 @@ def test_rows_of_each_number_of_threads(gpu_device, B, n, V, parts):
         if parts == "nothing":
             c.masks = c.tokens = c.bt = c.bv = c.ok = None
         c.check(c.run(), (0, n // 2, n - 1) if B < 100 else None)
+
+
+@pytest.mark.parametrize("B,V", [(256, 131_073), (256, 200_003), (260, 262_144), (256, 262_145)])
+def test_many_rows_of_large_vocabularies(gpu_device, B, V):
+    c = Call(B, 1, V, BF, V)
+    c.ok = None                                            # (a truth value for each token is all of the test's time)
+    got = c.run()
+    keep = [0, B // 2, B - 1]
+    for name in ("seen", "rep", "fre", "pre", "temp", "bt", "bv", "lens", "masks", "tokens"):
+        setattr(c, name, getattr(c, name)[keep])
+    c.B, c.logits = 3, c.logits[keep]
+    c.check(got[keep])
+
+
+@pytest.mark.parametrize("B,n,V", [(256, 1, 66_001), (800, 1, 4001), (300, 1, 20_001)])
+def test_rows_in_place(gpu_device, B, n, V):
+    c = Call(B, n, V, F32, 77)
+    c.lens[:] = n
+    ref, x = c.run(), c.logits.clone()
+    assert torch.equal(c.run(probs=x, logits=x), ref)
