@@ -541,16 +541,16 @@ __device__ __forceinline__ void write_soft(const Slice<E, THREADS, KIND> &s, flo
     });
 }
 
-// ... of a greedy one: nothing is read again
-template <bool NT, typename E, int THREADS, int KIND>
-__device__ __forceinline__ void write_greedy(const Slice<E, THREADS, KIND> &s, float *out, const Stat &a)
+// ... of tokens [x0, x1) of a greedy one: nothing is read again
+template <bool NT, int THREADS>
+__device__ __forceinline__ void write_greedy(float *out, int x0, int x1, int V, int32_t first)
 {
-    for (int at = s.x0 + (int)(threadIdx.x >> 6) * kBlock; at < s.x1; at += THREADS * kUnit) {
+    for (int at = x0 + (int)(threadIdx.x >> 6) * kBlock; at < x1; at += THREADS * kUnit) {
         const int x = at + 4 * (threadIdx.x & 63);
         float l[kUnit];
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) l[i] = token_of(x, i) == a.x ? 1.f : 0.f;
-        store_unit<NT>(out, x, s.p.V, at + kBlock <= s.x1, l);
+        for (int i = 0; i < kUnit; ++i) l[i] = token_of(x, i) == first ? 1.f : 0.f;
+        store_unit<NT>(out, x, V, at + kBlock <= x1, l);
     }
 }
 
@@ -559,13 +559,6 @@ __device__ __forceinline__ Stat thread_stat(const Slice<E, THREADS, KIND> &s, fl
 {
     return t > 0.f ? thread_stat_t<true>(s, w) : thread_stat_t<false>(s, w);
 }
-template <bool NT, typename E, int THREADS, int KIND>
-__device__ __forceinline__ void write_probs(const Slice<E, THREADS, KIND> &s, float *out, const Stat &a, float t, const Weight &w)
-{
-    if (t > 0.f) write_soft<NT>(s, out, a, w);
-    else write_greedy<NT>(s, out, a);
-}
-
 // Whether a row is one of its tree's
 __device__ __forceinline__ bool row_there(const ProbsParams &p, int64_t row)
 {
@@ -595,16 +588,25 @@ __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams
     __shared__ Stat s_stat[kThreads / 64];
     const int64_t row = blockIdx.x / p.slices;
     if (!row_there(p, row)) return;
-    const Slice<E, kThreads, KIND> s(p, row, (int)(blockIdx.x - row * p.slices), s_special, s_bits);
-    const float t = temperature_of(p, s.b);
+    const int slice = (int)(blockIdx.x - row * p.slices);
+    const float t = temperature_of(p, (int)(row / p.n));
     const Weight w(t > 0.f ? t : 1.f);
-    Stat a = kNoStat;
-    for (int i = threadIdx.x; i < p.slices; i += kThreads) {
-        const Stat part = ((const Stat *)p.stats)[row * p.slices + i];
-        merge(a, part.m, part.s, part.x, w);
+    float *out = p.probs + row * p.V;
+    auto stat = [&]() {
+        Stat a = kNoStat;
+        for (int i = threadIdx.x; i < p.slices; i += kThreads) {
+            const Stat part = ((const Stat *)p.stats)[row * p.slices + i];
+            merge(a, part.m, part.s, part.x, w);
+        }
+        return workgroup_stat<kThreads>(a, w, s_stat);
+    };
+    if (t > 0.f) {
+        const Slice<E, kThreads, KIND> s(p, row, slice, s_special, s_bits);
+        write_soft<NT>(s, out, stat(), w);
+    } else {
+        const int x0 = slice * p.slice_len;
+        write_greedy<NT, kThreads>(out, x0, x0 + p.slice_len < p.V ? x0 + p.slice_len : p.V, p.V, stat().x);
     }
-    a = workgroup_stat<kThreads>(a, w, s_stat);
-    write_probs<NT>(s, p.probs + row * p.V, a, t, w);
 }
 
 // A workgroup a row, in one launch: the row is read again for the probabilities, from a cache that holds what is under way.
@@ -620,7 +622,9 @@ __global__ __launch_bounds__(THREADS) void token_row_kernel(const ProbsParams p)
     const float t = temperature_of(p, s.b);
     const Weight w(t > 0.f ? t : 1.f);
     const Stat a = workgroup_stat<THREADS>(thread_stat(s, t, w), w, s_stat);
-    write_probs<NT>(s, p.probs + row * p.V, a, t, w);
+    float *out = p.probs + row * p.V;
+    if (t > 0.f) write_soft<NT>(s, out, a, w);
+    else write_greedy<NT, THREADS>(out, 0, p.V, p.V, a.x);
 }
 
 // ---- the record of a request's tokens -----------------------------------------------------------------------
