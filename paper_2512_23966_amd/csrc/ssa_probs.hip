@@ -592,12 +592,11 @@ __global__ __launch_bounds__(kThreads) void token_probs_kernel(const ProbsParams
     const float t = temperature_of(p, (int)(row / p.n));
     const Weight w(t > 0.f ? t : 1.f);
     float *out = p.probs + row * p.V;
+    const Stat *parts = (const Stat *)p.stats + row * p.slices;
+    Stat a = kNoStat;
+    if ((int)threadIdx.x < p.slices) a = parts[threadIdx.x];
     auto stat = [&]() {
-        Stat a = kNoStat;
-        for (int i = threadIdx.x; i < p.slices; i += kThreads) {
-            const Stat part = ((const Stat *)p.stats)[row * p.slices + i];
-            merge(a, part.m, part.s, part.x, w);
-        }
+        for (int i = threadIdx.x + kThreads; i < p.slices; i += kThreads) merge(a, parts[i].m, parts[i].s, parts[i].x, w);
         return workgroup_stat<kThreads>(a, w, s_stat);
     };
     if (t > 0.f) {
