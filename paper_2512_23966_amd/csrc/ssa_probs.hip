@@ -742,8 +742,8 @@ __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountP
 }  // namespace
 
 // A workgroup a row where there are many rows or they are short (up to 12,288 tokens, a row a 256 tokens, 256 rows), else slices: 2,048 workgroups in all as far as
-// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 10 and 12, 512 rows 18 and 24; 32,003,
-// 1 row 18 and 12, 64 rows 22 and 17, 128 rows 24 and 23; 131,072, 1 row 39 and 12, 128 rows 49 and 41, 256 rows 62 and 66, 512 rows 90 and 101.
+// there are 2,048 tokens for each, and two launches. With everything, us, row and slices: 8,000 tokens, 1 row 9 and 12, 512 rows 17 and 25; 32,003,
+// 1 row 17 and 12, 64 rows 21 and 16, 128 rows 23 and 23; 131,072, 1 row 39 and 12, 128 rows 49 and 41, 256 rows 62 and 65, 512 rows 91 and 96.
 void probs_plan(ProbsParams &p)
 {
     const int64_t rows = (int64_t)p.B * p.n;
@@ -762,11 +762,11 @@ static hipError_t launch_probs_t(const ProbsParams &p, hipStream_t stream)
     const dim3 grid((unsigned)((int64_t)p.B * p.n * p.slices));
     const size_t lds = p.masks || p.n_bias || p.allowed ? (size_t)(p.slice_len < p.V ? p.slice_len : p.V + 31) / 32 * 4 : 0;
     if (p.slices == 1) {
-        // Threads of a row, us with 256, 512 and 1,024 of them: 2,048 rows of 700 tokens 19, 29, 45, of 8,000 36, 45, 57, of 16,000 59, 62, 76; 256 rows of 8,000 15, 13, 13;
-        // 512 rows of 32,003 38, 33, 33; 256 rows of 131,072 102, 66, 62, 1,024 rows 235, 226, 212.
+        // Threads of a row, us with 256, 512 and 1,024 of them: 2,048 rows of 700 tokens 15, 26, 45, of 8,000 32, 40, 56; 1,024 rows of 8,000 24, 24, 36, of 16,000 35, 33, 48;
+        // 256 rows of 8,000 15, 13, 13; 512 rows of 32,003 38, 31, 32; 256 rows of 131,072 101, 66, 62, 1,024 rows, logits from memory, 235, 229, 212.
         // (65,535 trees of 64 rows of 1,024 threads are as many as a launch takes)
         static_assert(65535LL * kTreeNodes * 1024 <= 0xffffffffLL);
-        const int threads = p.V > 65536 ? 1024 : grid.x >= 768 && p.V <= 16384 ? 256 : 512;
+        const int threads = p.V > 65536 ? 1024 : grid.x >= 768 && p.V <= 8192 ? 256 : 512;
         if (threads == 1024) hipLaunchKernelGGL((token_row_kernel<E, 1024, KIND, NT>), grid, dim3(1024), lds, stream, p);
         else if (threads == 512) hipLaunchKernelGGL((token_row_kernel<E, 512, KIND, NT>), grid, dim3(512), lds, stream, p);
         else hipLaunchKernelGGL((token_row_kernel<E, 256, KIND, NT>), grid, dim3(256), lds, stream, p);

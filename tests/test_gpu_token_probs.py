@@ -349,7 +349,7 @@ def test_tokens_done_apart_side_by_side(gpu_device, B, n, V, dtype):
 
 
 @pytest.mark.parametrize("parts", ["all of it", "no record", "nothing"])
-@pytest.mark.parametrize("B,n,V", [(256, 1, 66_001), (4, 64, 131_072), (4, 64, 65_536), (800, 1, 16_384), (12, 64, 16_385), (800, 1, 1025), (400, 2, 513), (800, 1, 511)])
+@pytest.mark.parametrize("B,n,V", [(256, 1, 66_001), (4, 64, 131_072), (4, 64, 65_536), (800, 1, 16_384), (12, 64, 16_385), (800, 1, 8192), (768, 1, 8193), (800, 1, 1025), (400, 2, 513), (800, 1, 511)])
 def test_rows_of_each_number_of_threads(gpu_device, B, n, V, parts):
     for dtype in (BF, F32):
         c = Call(B, n, V, dtype, V, bias=9)
