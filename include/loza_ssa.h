@@ -710,7 +710,8 @@ int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int3
  * trimmed and trimmed_after: no request is. All calls change none of their inputs but those named, so they can be repeated; results may not overlap other
  * arrays of the call (LOZA_ERR_SHAPE). Numbers of requests out of range (lengths or held negative or beyond max_pages_per_seq pages): the request is left out.
  *
- * loza_ssa_pages_fork: request b becomes a copy of request from[b] (outside [0, B): no fork). Its place must be empty (cache_lens[b] and held[b] 0). It shares
+ * loza_ssa_pages_fork: request b becomes a copy of request from[b] (outside [0, B), or one whose numbers are out of range: no fork). Its place must be empty (cache_lens[b] and
+ * held[b] 0). It shares
  * the source's full pages and gets a new one for a page that is started, into which loza_ssa_pages_copy brings the rows; so neither writes where the other reads
  * as long as both only add rows. Several requests may have one source.
  *   cache_lens, held [B], free_pages, free_count, block_table: as loza_ssa_step_tables_held; entries of the forks' rows of block_table are written. New pages are dealt

@@ -73,7 +73,8 @@ __device__ __forceinline__ Fork fork_of(const ForkParams &p, int b)
     f.source = p.from[b];
     f.fits = f.source >= 0 && f.source < p.B && p.cache_lens[b] == 0 && p.held[b] == 0;
     f.rows = f.fits ? p.cache_lens[f.source] : 0;
-    if (f.rows < 0 || f.rows > (int64_t)p.max_pages << p.page_shift) f.fits = false;
+    const int held = f.fits ? p.held[f.source] : 0;
+    if (f.rows < 0 || f.rows > (int64_t)p.max_pages << p.page_shift || held < 0 || held > p.max_pages) f.fits = false;
     f.need = f.fits && (f.rows & (((int64_t)1 << p.page_shift) - 1)) != 0;
     return f;
 }
