@@ -556,6 +556,8 @@ int loza_ssa_norm_rope_f32(const float *x, const float *weight, const int32_t *p
  *     dx_c = r (h_c - x_c r^2 mean(h x)) there, g_c elsewhere;     dweight_c = sum over tokens and heads of g_c x_c r.
  *   x: what the forward call was given (not its result)     dx [T, H, d]: strided; dx == dout or dx == x with the same strides: in place. The row of a
  *           token with a negative position is left as it is, and adds nothing to dweight
+ *   A head whose squares add up to more than fp32 holds: 0 on the norm columns, and nothing to dweight. Elsewhere the sum of h x over a head's norm columns has to
+ *   fit fp32.
  *   dweight [norm_dim] fp32, overwritten; NULL: not wanted, and no workspace is needed
  *   workspace: loza_ssa_norm_rope_backward_workspace_bytes, 16-byte aligned, contents ignored; two calls that overlap in time need two
  * dweight's sums run in an order that depends on the sizes and the alignment alone, in fp32 within and in fp64 across workgroups.

@@ -311,7 +311,8 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(const NormParam
                     for (int e = 0; e < VEC; ++e) hw[j][u][e] = g[j][u][e] * lane.w[j][u][e];
             const float inv = 1.f / (float)n.norm_dim;
             const float r = 1.f / sqrtf(lane.dot(x, x, lanes) * inv + p.eps);
-            const float mean = lane.dot(hw, x, lanes) * inv * (r * r);
+            // (r is 0 where the squares add up to infinity: the result is 0 all around, whatever h x adds up to)
+            const float hx = lane.dot(hw, x, lanes), mean = r > 0.f ? hx * inv * (r * r) : 0.f;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
