@@ -32,7 +32,7 @@ constexpr int kMostSpecial = kTreeNodes + kMostBias;
 // next to another must not win by a rounding left out. Elsewhere (`soft`) a few units do not matter, and half of the instructions do.
 struct Change {
     float rep, inv, inv_lo, fre, pre;  // inv + inv_lo: 1 / rep
-    bool quick;                        // the division by `rep` as below
+    bool quick;                        // the division by `rep` as below (and what is said of small quotients there)
     bool repeats, counts, occurs;      // which of the three change anything: requests rarely ask for all of them (853 rows of 131,072, a sixth of them said: 215 -> 196 us)
 
     __device__ __forceinline__ void set(float rep_, float fre_, float pre_)
@@ -42,7 +42,7 @@ struct Change {
         inv_lo = __builtin_fmaf(-inv, rep_, 1.f) * inv;
         fre = fre_;
         pre = pre_;
-        quick = rep >= 0x1p-100f && rep <= 0x1p100f;
+        quick = rep >= 0x1p-20f && rep <= 0x1p20f && (fre_ == 0.f || fabsf(fre_) >= 0x1p-50f);
         repeats = rep_ != 1.f;
         counts = fre_ != 0.f;
         occurs = pre_ != 0.f || !(fabsf(fre_) < __builtin_inff());   // (infinity times 0 is not 0)
@@ -94,7 +94,8 @@ struct Change {
         return l;
     }
     // The same without branches of lanes. l / rep as l (inv + inv_lo), which is off by less than a unit, and a correction by what is left, fma(-q, rep, l) inv: that gives
-    // the rounded quotient (Markstein 1990; below 2^-100 it may miss by a step). One that overflows comes out as a NaN.
+    // the rounded quotient (Markstein 1990) where what is left is exact, which takes l and q of 2^-100 and more; with the repetitions that are `quick` a q of 2^-80 and more
+    // has both (smaller ones: small_matters). One that overflows comes out as a NaN.
     template <typename F>
     __device__ __forceinline__ void quickly(float (&l)[kUnit], F z) const
     {
@@ -120,6 +121,9 @@ struct Change {
             for (int i = 0; i < kUnit; ++i) l[i] -= (z(i) & 0x7fffu) != 0 ? pre : 0.f;
         }
     }
+    // Whether quotients of less than 2^-80, which may be off by a step, can decide which of a lane's tokens is the largest: not next to one of 2^-50 or more, before them or
+    // among them, nor where all are at -2^-50 or below. A penalty of 2^-50 or more leaves of them what it leaves of 0, and what a smaller one leaves is smaller than 2^-50.
+    __device__ __forceinline__ bool small_matters(float before, float largest) const { return before < 0x1p-50f && fabsf(largest) < 0x1p-50f; }
 };
 
 // exp(d / T) for d <= 0: 2^(d c), c = log2(e) / T. -infinity gives 0. Off by 2^-24 of |d| / T twice (the product, and c) and by the exponential's own unit.
@@ -349,26 +353,34 @@ struct Slice {
 #pragma unroll
                 for (int i = 0; i < kUnit; ++i) l[i] = settle(l[i]);
             } else {
-                // NaNs, or quotients: once more, from memory so that nothing is kept for this
-#pragma unroll 1
-                for (int i = 0; i < kUnit; ++i) {
-                    const int xi = token_of(x, i);
-                    float y = LOZA_NEG_INF;
-                    if (xi < p.V) {
-                        const uint32_t z = seen ? seen[xi] : 0u;
-                        y = settle(change.rounded(Elem<E>::get(row[xi]), z != 0, z & 0x7fffu));
-                    }
-#pragma unroll
-                    for (int k = 0; k < kUnit; ++k) l[k] = k == i ? y : l[k];
-                }
+                once_more(x, l);
             }
         }
-        if ((KIND != kPlain || !whole) && __any(raw.ok != 0xffu)) {
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) {
-                const uint32_t keep = (uint32_t)((int32_t)(raw.ok << (31 - i)) >> 31), y = __builtin_bit_cast(uint32_t, l[i]);
-                l[i] = __builtin_bit_cast(float, (y & keep) | (0xff800000u & ~keep));
+        if (KIND != kPlain || !whole) bar_tokens(raw, l);
+    }
+    // The changed logits of a lane's tokens from memory, so that nothing is kept for this: NaNs, and quotients that are not sure
+    __device__ __forceinline__ void once_more(int x, float (&l)[kUnit]) const
+    {
+#pragma unroll 1
+        for (int i = 0; i < kUnit; ++i) {
+            const int xi = token_of(x, i);
+            float y = LOZA_NEG_INF;
+            if (xi < p.V) {
+                const uint32_t z = seen ? seen[xi] : 0u;
+                y = settle(change.rounded(Elem<E>::get(row[xi]), z != 0, z & 0x7fffu));
             }
+#pragma unroll
+            for (int k = 0; k < kUnit; ++k) l[k] = k == i ? y : l[k];
+        }
+    }
+    // -inf for tokens done apart, not allowed, or not there
+    __device__ __forceinline__ static void bar_tokens(const Raw<E> &raw, float (&l)[kUnit])
+    {
+        if (!__any(raw.ok != 0xffu)) return;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) {
+            const uint32_t keep = (uint32_t)((int32_t)(raw.ok << (31 - i)) >> 31), y = __builtin_bit_cast(uint32_t, l[i]);
+            l[i] = __builtin_bit_cast(float, (y & keep) | (0xff800000u & ~keep));
         }
     }
     // Calls f(x, raw, whole) for this wave's blocks of 512 tokens; the next one's loads are under way meanwhile
@@ -463,7 +475,14 @@ __device__ __forceinline__ Stat thread_stat_t(const Slice<E, THREADS, KIND> &s, 
     s.units([&](int x, const Raw<E> &raw, bool whole) {
         float l[kUnit];
         s.template changed<SOFT>(x, whole, raw, l);
-        const float m = largest(l);
+        float m = largest(l);
+        if constexpr (!SOFT && KIND == kRecord) {
+            if (s.change.repeats && __any(s.change.small_matters(a.m, m))) {
+                s.once_more(x, l);
+                s.bar_tokens(raw, l);
+                m = largest(l);
+            }
+        }
         if (m > a.m) {
             if constexpr (SOFT) {
                 a.s *= w(a.m - m);
