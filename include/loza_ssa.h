@@ -678,7 +678,8 @@ int loza_ssa_keep_accepted(void *k_rows, void *v_rows, const int32_t *slots, con
  * (c > 0) presence; plus its bias; in fp32, in greedy rows each operation rounded by itself. Tokens that are not allowed, whatever their logits, and those whose result is a NaN, weigh
  * nothing. probs = exp((l - max) / temperature) / sum; where the temperature is not in [2^-100, 2^100] (0: greedy): 1 at the first of the largest. A row in
  * which nothing weighs is all 0 (loza_ssa_verify_tree then has no next token). Logits of +infinity share a row among them.
- * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30, as many rows as a launch takes. Sums in fp32, always in the same order.
+ * 1 <= n <= LOZA_TREE_MAX_NODES, B <= 65535, V <= 2^30, as many rows as a launch takes. Sums in fp32, always in the same order. Neither probs nor the workspace may lie on
+ * another array of the call (LOZA_ERR_SHAPE) but in place.
  */
 #define LOZA_MAX_BIAS 1024
 size_t loza_ssa_token_probs_workspace_bytes(int B, int n, int V);

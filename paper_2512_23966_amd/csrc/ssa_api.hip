@@ -1657,6 +1657,13 @@ static int token_probs(const void *logits, int64_t logits_row, const int32_t *tr
                             (const void *)temperature, (const void *)bias_tokens, (const void *)bias_values, (const void *)allowed, (const void *)probs})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(masks) & 7u) || !aligned16(seen) || !aligned16(workspace)) return LOZA_ERR_ALIGN;
+    // workgroups read what others' results would be written over (in place, a row is written by whoever has read it)
+    const int64_t rows = (int64_t)B * n, b4 = 4LL * B, bias = b4 * n_bias;
+    const bool in_place = logits == (const void *)probs;
+    const Span arrays[] = {{probs, rows * V * 4}, {workspace, rows * p.slices * 16}, {in_place ? nullptr : logits, ((rows - 1) * logits_row + V) * es}, {tree_lens, b4},
+                           {tokens, rows * 4}, {masks, rows * 8}, {seen, seen_row * 2 * B}, {repetition, b4}, {frequency, b4}, {presence, b4}, {temperature, b4},
+                           {n_bias ? bias_tokens : nullptr, bias}, {n_bias ? bias_values : nullptr, bias}, {allowed, rows * p.words * 4}};
+    if (overlap(arrays, 2, 14)) return LOZA_ERR_SHAPE;
     p.logits = logits; p.logits_row = logits_row; p.tree_lens = tree_lens; p.tokens = tokens; p.masks = masks; p.seen = seen; p.seen_row = seen_row;
     p.repetition = repetition; p.frequency = frequency; p.presence = presence; p.temperature = temperature;
     p.bias_tokens = bias_tokens; p.bias_values = bias_values; p.n_bias = n_bias; p.allowed = allowed; p.probs = probs; p.stats = (float *)workspace;

@@ -1,0 +1,21 @@
+"""Results of the calls beside the step that lie on other arrays of the call: refused before anything is launched. No GPU needed (the addresses are never read)."""
+import pytest
+
+from tests.test_beside_host import A, ERR_SHAPE, _probs
+
+INPUTS = ("logits", "lens", "tokens", "masks", "seen", "rep", "fre", "pre", "temp", "bt", "bv", "allowed")
+
+
+@pytest.mark.parametrize("fn", ["loza_ssa_token_probs", "loza_ssa_token_probs_f32"])
+def test_token_probs(fn):
+    at = {name: i * A for i, name in zip((1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12), INPUTS)}
+    for name in INPUTS[1:]:
+        assert _probs(fn, probs=at[name]) == ERR_SHAPE, name
+        assert _probs(fn, ws=at[name]) == ERR_SHAPE, name
+    es = 4 if fn.endswith("f32") else 2
+    # probabilities that begin inside the logits, or end there; the workspace on the logits' last row, on the probabilities' first and last
+    for bad in (dict(probs=A + 16), dict(probs=A + 16 * 1000 * es - 4), dict(probs=A - 16 * 1000 * 4 + 4), dict(ws=A), dict(ws=A + 16 * 1000 * es - 16), dict(ws=13 * A), dict(ws=13 * A + 16 * 4000 - 16),
+                dict(ws=13 * A - 240), dict(row=1100, probs=A + (15 * 1100 + 1000) * es - 4), dict(probs=A + 4 * 1000 * es)):
+        assert _probs(fn, **bad) == ERR_SHAPE, bad
+    if es == 4:                                              # (in place, but for the workspace)
+        assert _probs(fn, probs=A, ws=A + 64) == ERR_SHAPE
