@@ -701,6 +701,7 @@ int loza_ssa_token_probs_f32(const float *logits, int64_t logits_row, const int3
  *   fresh [B] int32 or NULL: where it is not 0, the request's row is cleared first (a new request, with its prompt and what it has said already)
  *   seen [B] rows, seen_row elements apart, as above
  * B <= 65535, n <= 2^30, V <= 2^30. The result does not depend on the order of the entries. Two calls that overlap in time must not have rows of seen in common.
+ * seen may not lie on another array of the call (LOZA_ERR_SHAPE).
  */
 int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int32_t *lens, const int32_t *prompt_lens, const int32_t *fresh,
                           uint16_t *seen, int64_t seen_row, int B, int n, int V, void *stream);

@@ -1696,6 +1696,9 @@ int loza_ssa_count_tokens(const int32_t *tokens, const int32_t *path, const int3
     for (const void *ptr : {(const void *)tokens, (const void *)path, (const void *)lens, (const void *)prompt_lens, (const void *)fresh})
         if (reinterpret_cast<uintptr_t>(ptr) & 3u) return LOZA_ERR_ALIGN;
     if (!aligned16(seen)) return LOZA_ERR_ALIGN;
+    const int64_t b4 = 4LL * B;
+    const Span arrays[] = {{seen, seen_row * 2 * B}, {tokens, b4 * n}, {path, b4 * n}, {lens, b4}, {prompt_lens, b4}, {fresh, b4}};
+    if (overlap(arrays, 1, 6)) return LOZA_ERR_SHAPE;
     const loza::CountParams p{tokens, path, lens, prompt_lens, fresh, seen, seen_row, B, n, V};
     return loza::launch_count_tokens(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }

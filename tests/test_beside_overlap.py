@@ -1,7 +1,7 @@
 """Results of the calls beside the step that lie on other arrays of the call: refused before anything is launched. No GPU needed (the addresses are never read)."""
 import pytest
 
-from tests.test_beside_host import A, ERR_SHAPE, _probs
+from tests.test_beside_host import A, ERR_SHAPE, B, _probs
 
 INPUTS = ("logits", "lens", "tokens", "masks", "seen", "rep", "fre", "pre", "temp", "bt", "bv", "allowed")
 
@@ -19,3 +19,14 @@ def test_token_probs(fn):
         assert _probs(fn, **bad) == ERR_SHAPE, bad
     if es == 4:                                              # (in place, but for the workspace)
         assert _probs(fn, probs=A, ws=A + 64) == ERR_SHAPE
+
+
+def test_count_tokens():
+    def call(**k):
+        a = dict(tokens=A, path=2 * A, lens=3 * A, prompt=4 * A, fresh=5 * A, seen=6 * A, row=1000, B=2, n=8, V=1000)
+        a.update(k)
+        return B.lib().loza_ssa_count_tokens(*a.values(), None)
+    for i in range(1, 6):
+        assert call(seen=i * A) == ERR_SHAPE, i
+        assert call(seen=i * A - 2 * 1000 * 2 + 16) == ERR_SHAPE, i
+    assert call(tokens=6 * A + 2 * 1000 * 2 - 4) == ERR_SHAPE
