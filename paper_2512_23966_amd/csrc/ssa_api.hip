@@ -1753,6 +1753,9 @@ int loza_ssa_pages_copy(void *k_pages, void *v_pages, const int32_t *from, const
     if (num_pages > all || n > all) return LOZA_ERR_SHAPE;
     if (!aligned16(k_pages) || !aligned16(v_pages)) return LOZA_ERR_ALIGN;
     if (int rc = check_ints({from, to, rows, count})) return rc;
+    const int64_t pages = n_layers * num_pages * page_size;                                // (a quarter of 2^63 bytes at most, by the above)
+    const Span arrays[] = {{k_pages, pages * k_row_bytes}, {v_pages, v_pages ? pages * v_row_bytes : 0}, {from, 4 * n}, {to, 4 * n}, {rows, 4 * n}, {count, 4}};
+    if (overlap(arrays, 2, 6)) return LOZA_ERR_SHAPE;
     const loza::CopyParams p{(char *)k_pages, (char *)v_pages, from, to, rows, count, n, num_pages, k_row_bytes, v_pages ? v_row_bytes : 0, n_layers, page_size};
     return loza::launch_pages_copy(p, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }

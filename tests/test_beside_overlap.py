@@ -30,3 +30,17 @@ def test_count_tokens():
         assert call(seen=i * A) == ERR_SHAPE, i
         assert call(seen=i * A - 2 * 1000 * 2 + 16) == ERR_SHAPE, i
     assert call(tokens=6 * A + 2 * 1000 * 2 - 4) == ERR_SHAPE
+
+
+def test_pages_copy():
+    """The pages of keys and values, and the lists, lie apart."""
+    def call(**k):
+        a = dict(k=100 * A, v=200 * A, src=3 * A, dst=4 * A, rows=5 * A, count=6 * A, n=3, layers=2, pages=100, page=64, kb=1152, vb=256)
+        a.update(k)
+        return B.lib().loza_ssa_pages_copy(*a.values(), None)
+    k_bytes, v_bytes = 2 * 100 * 64 * 1152, 2 * 100 * 64 * 256
+    for bad in (dict(v=100 * A + 16), dict(v=100 * A + k_bytes - 16), dict(v=100 * A - v_bytes + 16), dict(v=100 * A + 1152 * 64 * 100)):
+        assert call(**bad) == ERR_SHAPE, bad
+    for name in ("src", "dst", "rows", "count"):
+        for bad in (100 * A, 100 * A + k_bytes - 4, 200 * A, 200 * A + v_bytes - 4):
+            assert call(**{name: bad}) == ERR_SHAPE, (name, bad)
