@@ -541,7 +541,8 @@ int loza_ssa_rope_append_f32(const float *q, const float *k, const float *v, con
  * loza_ssa_rope rotates them. The two ranges may be apart (a latent row: 512 normed columns, 64 rotated ones), the same (heads of width 128), or overlap.
  *   weight [norm_dim] fp32, NULL: ones     1 <= norm_dim, d <= LOZA_NORM_MAX_DIM; eps: a positive normal number
  *   everything else, padding, strides and in-place calls among it: as loza_ssa_rope. A head whose squares add up to more than fp32 holds gives 0.
- * Sums in fp32, one rounding of each result. All heads have the one weight.
+ * Sums in fp32, one rounding of each result. All heads have the one weight. In these calls, the gradient and loza_ssa_norm_rope_append, a result (a workspace, a cache) without gaps
+ * that lies on another such array of the call, and is not in place, is refused (LOZA_ERR_SHAPE); that of strided ones is the caller's to know.
  */
 #define LOZA_NORM_MAX_DIM 1024
 int loza_ssa_norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,

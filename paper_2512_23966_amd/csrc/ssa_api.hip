@@ -1493,6 +1493,13 @@ static int check_norm_heads(const loza::NormHeads &n, int64_t T, int rot, int es
     return (reinterpret_cast<uintptr_t>(n.w) & 3u) ? LOZA_ERR_ALIGN : LOZA_OK;
 }
 
+// The place of [T, H, d] where it has no gaps; strided rows share their buffers (slices of all projections of a token): none
+static Span dense_span(const void *ptr, int64_t T, int H, int d, int64_t token, int64_t head, int es)
+{
+    const bool dense = ((H == 1 || head == d) && (T == 1 || token == (int64_t)H * d)) || ((T == 1 || token == d) && (H == 1 || head == T * d));
+    return {dense ? ptr : nullptr, sat_mul(T, (int64_t)H * d * es)};
+}
+
 static int norm_rope(const void *x, const float *weight, const int32_t *positions, const double *freq, void *out, int64_t T, int H, int d,
                      int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head, int norm_begin, int norm_dim, float eps,
                      int rot_begin, int rot_dim, int interleaved, float mscale, int es, void *stream)
@@ -1503,6 +1510,9 @@ static int norm_rope(const void *x, const float *weight, const int32_t *position
     if (int rc = check_norm_call(p, true)) return rc;
     if (int rc = check_norm_heads(p.q, T, rot_dim, es, true)) return rc;
     if (norm_dim < 1) return LOZA_ERR_SHAPE;
+    const Span arrays[] = {dense_span(out, T, H, d, out_token, out_head, es), dense_span(x == out ? nullptr : x, T, H, d, x_token, x_head, es),
+                           {weight, 4LL * norm_dim}, {positions, 4 * T}, {freq, 4LL * rot_dim}};
+    if (overlap(arrays, 1, 5)) return LOZA_ERR_SHAPE;
     return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }
 
@@ -1549,6 +1559,11 @@ static int norm_rope_backward(const void *dout, const void *x, const float *weig
         if (!aligned16(workspace)) return LOZA_ERR_ALIGN;
         p.partial = (float *)workspace;
     }
+    const Span arrays[] = {dense_span(dx, T, H, d, dx_token, dx_head, es), {dweight, 4LL * norm_dim},
+                           {p.partial, dweight ? (int64_t)loza_ssa_norm_rope_backward_workspace_bytes(T, H, d, norm_dim) : 0},
+                           dense_span(dout == dx ? nullptr : dout, T, H, d, dout_token, dout_head, es), dense_span(x == dx ? nullptr : x, T, H, d, x_token, x_head, es),
+                           {weight, 4LL * norm_dim}, {positions, 4 * T}, {freq, 4LL * rot_dim}};
+    if (overlap(arrays, 3, 8)) return LOZA_ERR_SHAPE;
     return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }
 
@@ -1593,6 +1608,12 @@ static int norm_rope_append(const void *q, const float *q_weight, const void *k,
             v == v_rows) return LOZA_ERR_SHAPE;
         if ((reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(v_rows)) & (uintptr_t)(es - 1)) return LOZA_ERR_ALIGN;
     }
+    // (new rows may be in the cache already, elsewhere than where they go)
+    const Span arrays[] = {q ? dense_span(q_out, T, Hq, d_q, q_out_token, q_out_head, es) : Span{nullptr, 0}, {k_rows, sat_mul(cache_rows, (int64_t)Hkv * d_k * es)},
+                           {v_rows, v ? sat_mul(cache_rows, (int64_t)Hkv * d_v * es) : 0}, q && q != q_out ? dense_span(q, T, Hq, d_q, q_token, q_head, es) : Span{nullptr, 0},
+                           {q && q_norm_dim ? q_weight : nullptr, 4LL * q_norm_dim}, {k_norm_dim ? k_weight : nullptr, 4LL * k_norm_dim}, {positions, 4 * T},
+                           {slots, 4 * T}, {freq, 4LL * rot_dim}};
+    if (overlap(arrays, 3, 9)) return LOZA_ERR_SHAPE;
     return loza::launch_norm_rope(p, es, (hipStream_t)stream) == hipSuccess ? LOZA_OK : LOZA_ERR_HIP;
 }
 

@@ -1,7 +1,7 @@
 """Results of the calls beside the step that lie on other arrays of the call: refused before anything is launched. No GPU needed (the addresses are never read)."""
 import pytest
 
-from tests.test_beside_host import A, ERR_SHAPE, B, _probs
+from tests.test_beside_host import A, ERR_SHAPE, B, _append, _back, _norm, _probs
 
 INPUTS = ("logits", "lens", "tokens", "masks", "seen", "rep", "fre", "pre", "temp", "bt", "bv", "allowed")
 
@@ -44,3 +44,32 @@ def test_pages_copy():
     for name in ("src", "dst", "rows", "count"):
         for bad in (100 * A, 100 * A + k_bytes - 4, 200 * A, 200 * A + v_bytes - 4):
             assert call(**{name: bad}) == ERR_SHAPE, (name, bad)
+
+
+def test_norm_rope():
+    """Results whose rows lie one behind the other, and dense inputs; strided ones share their buffers (slices of a row of all projections), and are the caller's."""
+    for name in ("w", "pos", "freq"):
+        assert _norm(**{name: 5 * A}) == ERR_SHAPE, name
+    assert _norm(out=A + 16) == ERR_SHAPE and _norm(out=A - 16) == ERR_SHAPE and _norm("loza_ssa_norm_rope_f32", out=A + 16) == ERR_SHAPE
+    for name, at in (("dout", 6 * A), ("x", A), ("w", 2 * A), ("pos", 3 * A), ("freq", 4 * A), ("dx", 5 * A), ("dw", 7 * A)):
+        assert _back(ws=at) == ERR_SHAPE, name
+        assert name == "dw" or _back(dw=at) == ERR_SHAPE, name
+        assert name not in ("w", "pos", "freq") or _back(dx=at) == ERR_SHAPE, name
+    assert _back(dx=6 * A + 16) == ERR_SHAPE and _back(dx=A + 16) == ERR_SHAPE and _back(dx=A - 16) == ERR_SHAPE
+    assert _back(ws=7 * A - 5 * 64 * 4 + 16) == ERR_SHAPE
+
+
+def test_norm_rope_append():
+    for name in ("wq", "wk", "pos", "slots", "freq"):
+        for result in (9 * A, 10 * A, 11 * A):
+            assert _append(**{name: result}) == ERR_SHAPE, (name, result)
+    cache = 100 * 2 * 64 * 2
+    for bad in (dict(k_rows=11 * A), dict(v_rows=10 * A + cache - 16), dict(v_rows=10 * A - cache + 16), dict(q_out=10 * A), dict(q_out=11 * A + 16), dict(q_out=A + 16), dict(q=10 * A)):
+        assert _append(**bad) == ERR_SHAPE, bad
+
+
+def test_the_largest_sizes():
+    """Numbers of bytes that pass 64 bits: as many as there are."""
+    far = 1 << 40
+    assert _norm("loza_ssa_norm_rope_f32", T=(1 << 31) - 1, H=1 << 20, d=1024, xt=1 << 30, xh=1024, ot=1 << 30, oh=1024, out=A, x=A + 4 * far) == ERR_SHAPE
+    assert _append("loza_ssa_norm_rope_append_f32", rows=(1 << 31) - 1, Hkv=1 << 20, dk=1024, kh=1024, kt=1 << 30, dv=1024, vh=1024, vt=1 << 30, k_rows=10 * A, v_rows=10 * A + 4 * far) == ERR_SHAPE
