@@ -6,12 +6,14 @@
 //     dx_c = r (h_c - x_c r^2 mean(h x)) there, g_c elsewhere,     dw_c = the sum over tokens and heads of g_c x_c r,
 // r formed again from x, which is read anyway. All of it in fp32, one rounding of each result.
 //
-// What bounds it: memory, once there are a few thousand heads: 16,384 tokens of 32 heads of 128 columns 53 us, 5.1 TB/s, and back 70 + 5 (a 1 GiB copy runs at 5.1);
-// 8,192 tokens of the wide shape into the cache 36 us, 4.2 TB/s (128-byte pieces of rows of 1,152); 64 tokens of 40 heads 5 us, all latency. A head
+// What bounds it: memory, once there are a few thousand heads: 16,384 tokens of 32 heads of 128 columns 53 us, 5.1 TB/s, and back 70 + 5 (a 1 GiB copy runs at 5.1), in fp32 106,
+// 5.1 TB/s, and 157 with the launch that adds; 8,192 tokens of the wide shape into the cache 36 us, 4.2 TB/s (128-byte pieces of rows of 1,152), in fp32 68, 4.5 TB/s; 64 tokens of
+// 40 heads 5 us, all latency. A head
 // belongs to a group of 8 to 64 lanes of one wave (4 for the narrowest), each with two units of 16 bytes: of rotary columns in half layout
 // the two ends of the same pairs, of others any two. So sums are a few exchanges between lanes, a pair is in one lane, and since a lane has the
 // same columns of every head it takes, weights and their gradients stay in registers. Rows of 72 units (576 columns) leave 28 of 64 lanes
-// idle: 16,384 of them, one a token, 16 us, 2.3 TB/s, of which the angles, 32 in 64 bits for each row, are a good part.
+// idle: 16,384 of them, one a token, 15 us, 2.5 TB/s, and back 24 (fp32, two items a lane: 17, 4.5 TB/s, and 29). A workgroup has one chunk of 8 of them there: its angles, 32 in 64 bits
+// a token, wait for its positions, and a group has two rows in all.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -3,7 +3,7 @@
 // A page belongs to the requests whose rows of the block table name it: one, and as many more as shared[page] says. Numbers of holders
 // are changed by integer atomics, whose order does not show; lists are written in the order of requests or of page numbers, by counting
 // what comes before. What bounds all of it but the copies: the latency of a few launches and of the loads in them that wait for each other (256 requests on 30,000
-// pages: fork 2 + 5 us, give back 3 + 6 + 6; 40,000 pages renamed 5 + 6 + 9 + 7). The copies run at the memory's rate: 9,900 pages of 36 KB 148 us, 4.9 TB/s.
+// pages: fork 2 + 5 us, give back 3 + 6 + 6; 40,000 pages renamed 5 + 6 + 9 + 7). The copies run at the memory's rate: 9,900 pages of 36 KB 147 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -28,7 +28,7 @@ __device__ __forceinline__ int64_t valid_count(const int32_t *count, int64_t num
     return c < 0 ? 0 : c < num_free ? c : num_free;
 }
 
-// Numbers before this thread's in a workgroup of 1,024 (each 0 .. 4)
+// Numbers before this thread's in a workgroup of 1,024 (each 0 .. 32: pages, or the bits of a word of them)
 __device__ __forceinline__ int scan_before(int x, int32_t *lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -5,8 +5,8 @@
 //     l' = l / repetition if l > 0, l * repetition otherwise, where it occurred;  l'' = l' - frequency c - presence (c > 0) + bias
 // and no weight where the grammar does not allow it (or l'' is a NaN); p = exp((l'' - max) / T) / sum, or 1 at the first of the largest.
 //
-// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 168 us, 4.8 TB/s); with everything the vector ALU as well,
-// 39 instructions a token in two passes (the same, 853 of the rows alive: 212 us, 150 where a cache has the logits; the memory's part is 136). All of it is done
+// What bounds it: memory without penalties, 4 bytes a token out and 2 or 4 in (1,024 rows of 131,072 bf16 logits 169 us, 4.8 TB/s, fp32 251, 4.3 TB/s); with everything the vector ALU
+// as well, 39 instructions a token in two passes (bf16, 853 of the rows alive: 210 us, 159 where a cache has the logits; the memory's part is 136). All of it is done
 // on the way. The tokens of a tree's own nodes and the biased ones are a few hundred of 100,000: the pass over the row leaves
 // them out (a bit each in LDS), and a thread each does them apart, so that the pass looks nothing up.
 #include <hip/hip_runtime.h>
@@ -688,8 +688,9 @@ __global__ __launch_bounds__(256) void count_tokens_kernel(const CountParams p)
 }
 
 // The same for many tokens: a workgroup takes a slice of a request's row, counts in LDS (bit 31: in the prompt) what of all tokens falls into it, and
-// writes the units of 8 that changed. Every slice reads all tokens, out of L2, four loads of four under way (16 requests of 100,000 tokens 12.7 us, 14.5 with slices of 16,384,
-// 19.5 with a load at a time).
+// writes the units of 8 that changed. Every slice reads all tokens, four loads of four under way (16 requests of 100,000 tokens 12.4 us, 14.5 with slices of 16,384, 19.5 with a load
+// at a time). That reading is what it takes: 10.5 us without the comparisons and the counting, 11.0 with the comparisons. Each request's slices lie on all 8 dies, so each die's L2 (4 MB)
+// asks for the 6.4 MB of all requests, 55 MB in all, and half of the 875,000 requests to L2 miss. How the tokens are spread does not show (evenly, or half of them in one slice: 12.4).
 constexpr int kCountSlice = 8192, kCountThreads = 1024;
 
 __global__ __launch_bounds__(kCountThreads) void count_slice_kernel(const CountParams p)
@@ -800,7 +801,8 @@ static hipError_t launch_probs_t(const ProbsParams &p, hipStream_t stream)
 template <typename E, int KIND>
 static hipError_t launch_probs_p(const ProbsParams &p, hipStream_t stream)
 {
-    // Results that no cache holds are stored past the caches, which keep the logits for their second reading (1,024 rows of 131,072 bf16 logits 244 -> 162 us)
+    // Results that no cache holds are stored past the caches, which keep the logits for their second reading (1,024 rows of 131,072 logits, us: bf16 197 -> 169, with a record
+    // 227 -> 213; fp32 287 -> 251 and 305 -> 276)
     return (int64_t)p.B * p.n * p.V * 4 >= 128 << 20 ? launch_probs_t<E, KIND, true>(p, stream) : launch_probs_t<E, KIND, false>(p, stream);
 }
 
@@ -816,8 +818,10 @@ hipError_t launch_token_probs(const ProbsParams &p, int elem_bytes, hipStream_t 
     return elem_bytes == 2 ? launch_probs_e<uint16_t>(p, stream) : launch_probs_e<float>(p, stream);
 }
 
-// Entries by slices from here on, where the row is no longer than a million. 16 requests, us, an entry a thread and slices: 131,072 tokens, 64 entries 2.5 and 3.8, 512 of
-// them 3.5 and 4.2, 8,192 20 and 5; with one in 20 the same token 3.6 and 3.9, 12.9 and 4.1, 555 and 5. A million tokens, 512 entries 3 to 13 and 8; four million 3 to 13 and 21.
+// Entries by slices from here on, where the row is no longer than a million. 16 requests, 131,072 tokens, us, an entry a thread and slices: 256 entries 2.5 and 3.1 where they are
+// spread evenly, 4.4 and 3.1 where half are one of 8,192 tokens, 9.0 and 3.0 where one in 20 is the same; 512 of them 2.8 and 3.2, 7.0 and 3.1, 16.4 and 3.1; 2,048 3.6 and 3.4 and, of
+// few tokens, 21 and 3.3. So it is the few entries of a frequent token, which texts have, that decide; evenly spread ones lose half a microsecond up to 1,000. 64 entries: 2.5 and 3.8. A
+// million tokens, 512 entries 3 to 13 and 8; four million 3 to 13 and 21.
 constexpr int kManyTokens = 256;
 
 hipError_t launch_count_tokens(const CountParams &p, hipStream_t stream)
